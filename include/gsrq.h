@@ -51,7 +51,8 @@ typedef enum {
   GSRQ_E_HIP = 4           /* a HIP runtime call failed                    */
 } gsrq_status;
 
-typedef enum { GSRQ_F32 = 0, GSRQ_F16 = 1 } gsrq_dtype;
+/* GSRQ_BF16: the paged cache's entry points only. */
+typedef enum { GSRQ_F32 = 0, GSRQ_F16 = 1, GSRQ_BF16 = 2 } gsrq_dtype;
 
 /* Problem shape.  N rows of D elements, subvector dimension d (d divides D,
  * G = D/d subspaces), K codewords per codebook (power of two), M stages. */
@@ -389,6 +390,106 @@ gsrq_status gsrq_attn_decode_noalloc(const gsrq_attn_shape* a, const gsrq_shape*
                                      const float* v_shape, const void* q, gsrq_dtype q_dtype,
                                      float* out, void* stream);
 
+/*
+ * The paged cache: keys and values of every token as they are, in pages of a
+ * pool that sequences share.  A program that serves a model keeps the tokens
+ * of a prompt here while it attends to them, codes what it keeps for longer
+ * (gsrq_encode takes the rows of [N][D] before their rotation), and brings a
+ * coded session back into pages when it goes on.
+ *
+ * Token t of sequence b lies in page table[b][t / page_size], at place
+ * t % page_size.  Elements of a head are adjacent; pages, tokens and heads
+ * lie at any strides (in elements), so pools [pages][page_size][Hkv][head_dim]
+ * and [pages][Hkv][page_size][head_dim] are both taken.  A table entry outside
+ * [0, pages) stands for a page that is not there: nothing is written to its
+ * tokens, and nobody attends to them.  A page may stand in several rows of the
+ * table (a shared prompt); a call that writes one token of a page from two
+ * rows leaves either.
+ * This build: head_dim 64, 128 or 256, page_size a power of two, float16 or
+ * bfloat16 pages (other valid shapes GSRQ_E_UNSUPPORTED); k and v 16-byte
+ * aligned, strides multiples of 8 elements.
+ */
+typedef struct {
+  void* k;                 /* key pages                                       */
+  void* v;                 /* value pages                                     */
+  int64_t k_stride[3];     /* elements from page to page, token to token and  */
+  int64_t v_stride[3];     /* head to head                                    */
+  const int32_t* table;    /* [B][ldt] pages of every sequence in order       */
+  int64_t ldt;             /* entries from row to row of the table (>= per)   */
+  int32_t pages;           /* pages in the pool                               */
+  int32_t page_size;       /* tokens per page                                 */
+  int32_t per;             /* table entries per sequence                      */
+  int32_t B;               /* sequences                                       */
+  int32_t Hkv;             /* key/value heads                                 */
+  int32_t head_dim;        /* elements per head                               */
+  gsrq_dtype dtype;        /* of the pages                                    */
+} gsrq_pages;
+
+/* Rows [T][heads][head_dim] at any strides (in elements; multiples of 16
+ * bytes, the first row 16-byte aligned). */
+typedef struct {
+  const void* data;
+  int64_t token_stride, head_stride;
+} gsrq_heads;
+
+/*
+ * gsrq_paged_append -- put the keys and values of new tokens into their
+ * pages, with the norms of the heads and the position rotation on the way;
+ * the tokens' queries take the same norms and rotation.
+ *
+ * The T rows of a call hold the new tokens of all sequences one after
+ * another: sequence b owns rows q_start[b] .. q_start[b+1] - 1, and
+ * seq_len[b] counts its tokens with the new ones, so row q_start[b] + i is at
+ * position p = seq_len[b] - (q_start[b+1] - q_start[b]) + i.  Rows of no
+ * sequence are left out, and so are keys and values at a position that the
+ * table does not hold.  For every head x of a row
+ *   y = x / sqrt(mean(x^2) + eps) * norm        (with a norm; values have none)
+ *   key, query = R_p y                          (with theta)
+ * where R_p turns elements j and j + head_dim/2 together by the angle
+ * p * theta[j] (rotate-half form, as gsrq_attn_decode).  Norms and rotations
+ * are float32, angles float64; results are rounded once.
+ *
+ *  q_start           [B + 1] int32, ascending, inside [0, T].
+ *  seq_len           [B] int32.
+ *  k, v              [T][Hkv][head_dim] rows, q [T][Hq][head_dim] rows or NULL,
+ *                    all of `dtype` (float32, float16 or bfloat16).
+ *  theta             [head_dim / 2] float64 angles per position (for base b:
+ *                    b^(-2j / head_dim)), or NULL: nothing is turned.
+ *  k_norm, q_norm    [head_dim] float32 norm weights, or NULL.
+ *  eps               >= 0.
+ *  q_out             [T][Hq][head_dim] of the pages' type, 16-byte aligned;
+ *                    NULL when q is.  May be q itself where the types agree
+ *                    and q is dense.
+ */
+gsrq_status gsrq_paged_append(const gsrq_pages* pages, int64_t T, const int32_t* q_start,
+                              const int32_t* seq_len, const gsrq_heads* k, const gsrq_heads* v,
+                              const gsrq_heads* q, int32_t Hq, gsrq_dtype dtype,
+                              const double* theta, const float* k_norm, const float* q_norm,
+                              float eps, void* q_out, void* stream);
+
+/*
+ * gsrq_paged_restore -- decode a coded context into pages: tokens
+ * 0 .. seq_len[b] - 1 of every sequence, values as gsrq_decode gives them and
+ * keys turned at their positions by theta as gsrq_paged_append does (keys are
+ * coded before their rotation).  Each stage's codeword is rounded to float32,
+ * the stages are summed in float32 in stage order, and the result (keys:
+ * after a float32 rotation) is rounded once to the pages' type.
+ *
+ *  kv                code shape: D = Hkv * head_dim, d >= 8, any K, M that
+ *                    gsrq_decode takes.
+ *  cap               code rows per sequence; seq_len is held inside [0, cap].
+ *  k_codes, v_codes  [B][cap][gsrq_code_words(kv)] uint32 (kv->N >= B * cap).
+ *  seq_len           [B] int32.
+ *  k_gain, k_shape   codebooks [M][G][K], [M][G][K][d], shapes 16-byte aligned.
+ *  v_gain, v_shape
+ *  theta             as above, or NULL: keys are stored as coded.
+ */
+gsrq_status gsrq_paged_restore(const gsrq_pages* pages, const gsrq_shape* kv, int32_t cap,
+                               const uint32_t* k_codes, const uint32_t* v_codes,
+                               const int32_t* seq_len, const float* k_gain, const float* k_shape,
+                               const float* v_gain, const float* v_shape, const double* theta,
+                               void* stream);
+
 /* Kernel kinds reported by the optional launch timing below. */
 enum {
   GSRQ_KERNEL_ASSIGN = 0,     /* fused assignment + weighted accumulation */
@@ -396,13 +497,14 @@ enum {
                               /* the previous iteration's codebook update)  */
   GSRQ_KERNEL_FINALIZE = 1,   /* codebook update + operand tiles          */
   GSRQ_KERNEL_ENCODE = 2,     /* stage-fused encoder                      */
-  GSRQ_KERNEL_DECODE = 3,     /* gather-sum decoder                       */
+  GSRQ_KERNEL_DECODE = 3,     /* gather-sum decoder, restoring into pages */
   GSRQ_KERNEL_TRANSPOSE = 4,  /* subspace-major copy / seeding of the input */
   GSRQ_KERNEL_ACCUMULATE = 5, /* weighted sums per codeword slice (d > 8)  */
   GSRQ_KERNEL_FRAGMENTS = 6,  /* operand fragment tables (d > 8 or K > 256) */
   GSRQ_KERNEL_EXACT = 7,      /* float64 rescoring of deferred rows         */
-  GSRQ_KERNEL_ATTENTION = 8,  /* decode attention over a coded cache       */
-  GSRQ_KERNEL_KINDS = 9
+  GSRQ_KERNEL_ATTENTION = 8,  /* attention over a coded or paged cache     */
+  GSRQ_KERNEL_APPEND = 9,     /* appending to a paged cache                */
+  GSRQ_KERNEL_KINDS = 10
 };
 
 /* Measurement hook, the library's only process state.  While enabled, every

@@ -7,6 +7,7 @@ functions from here raises instead of falling back to anything else.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -19,7 +20,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libgsrq.so")
 
 GSRQ_OK, GSRQ_E_ARG, GSRQ_E_UNSUPPORTED, GSRQ_E_WORKSPACE, GSRQ_E_HIP = range(5)
-GSRQ_F32, GSRQ_F16 = 0, 1
+GSRQ_F32, GSRQ_F16, GSRQ_BF16 = 0, 1, 2
 GSRQ_RESUME, GSRQ_ASSIGN_IN, GSRQ_NO_EARLY_STOP, GSRQ_KMEANS, GSRQ_CHECK_INPUTS = 1, 2, 4, 8, 16
 
 
@@ -39,6 +40,19 @@ class AttnShape(ctypes.Structure):
                 ("Hkv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("rope_base", ctypes.c_float), ("scale", ctypes.c_float),
                 ("flags", ctypes.c_uint32)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_stride", ctypes.c_int64 * 3),
+                ("v_stride", ctypes.c_int64 * 3), ("table", ctypes.c_void_p),
+                ("ldt", ctypes.c_int64), ("pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("per", ctypes.c_int32), ("B", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -99,6 +113,13 @@ def load_library(path: str = LIB_PATH):
     lib.gsrq_attn_decode_noalloc.restype = ctypes.c_int
     lib.gsrq_attn_decode_noalloc.argtypes = [AP, SP, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                              ctypes.c_int, _vp, _vp]
+    PP, HP = ctypes.POINTER(Pages), ctypes.POINTER(Heads)
+    lib.gsrq_paged_append.restype = ctypes.c_int
+    lib.gsrq_paged_append.argtypes = [PP, ctypes.c_int64, _vp, _vp, HP, HP, HP, ctypes.c_int32,
+                                      ctypes.c_int, _vp, _vp, _vp, ctypes.c_float, _vp, _vp]
+    lib.gsrq_paged_restore.restype = ctypes.c_int
+    lib.gsrq_paged_restore.argtypes = [PP, SP, ctypes.c_int32, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                       _vp, _vp]
     lib.gsrq_timing_enable.restype = ctypes.c_int
     lib.gsrq_timing_enable.argtypes = [ctypes.c_int]
     lib.gsrq_timing_enable_kinds.restype = ctypes.c_int
@@ -111,7 +132,7 @@ def load_library(path: str = LIB_PATH):
 
 
 KERNEL_KINDS = ("assign", "finalize", "encode", "decode", "transpose", "accumulate",
-                "fragments", "exact", "attention")
+                "fragments", "exact", "attention", "append")
 
 
 def timing_enable(on: bool = True, kinds=None):
@@ -522,3 +543,149 @@ def attn_decode(k_codes, v_codes, seq_len, k_gain, k_shape, v_gain, v_shape, q, 
                               ws.numel() * ws.element_size(), _stream_handle(stream))
     _check(st, "gsrq_attn_decode")
     return out
+
+
+# ------------------------------------------------------------- paged cache
+
+def _paged_dtype(t, name) -> int:
+    torch = _torch()
+    if t.dtype == torch.bfloat16:
+        return GSRQ_BF16
+    try:
+        return _dtype_code(t)
+    except TypeError:
+        raise TypeError(f"{name} must be float16, bfloat16 or float32, not {t.dtype}") from None
+
+
+def _on(device, stream):
+    """Context of a paged call: its stream's device is current and its new
+    tensors come from its stream's memory, so that a workspace freed when the
+    call returns is not handed to another stream while it is in use."""
+    torch = _torch()
+    if device.type != "cuda":
+        raise ValueError(f"the tensors are on {device}, expected a GPU")
+    if stream is None:
+        if device.index == torch.cuda.current_device():
+            return contextlib.nullcontext()
+        return torch.cuda.device(device)
+    if stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+    return torch.cuda.stream(stream)
+
+
+def _pages(k_pages, v_pages, table) -> Pages:
+    torch = _torch()
+    if k_pages.dim() != 4 or v_pages.shape != k_pages.shape:
+        raise ValueError("k_pages and v_pages must be [pages, page_size, Hkv, head_dim], both alike")
+    dev = k_pages.device
+    if k_pages.dtype not in (torch.float16, torch.bfloat16) or v_pages.dtype != k_pages.dtype:
+        raise TypeError("pages must be float16 or bfloat16, both alike")
+    if table.dim() != 2 or table.dtype != torch.int32:
+        raise TypeError("table must be a 2-D int32 tensor")
+    if v_pages.device != dev or table.device != dev:
+        raise ValueError(f"v_pages and table must be on {dev}")
+    ks, vs, ts = k_pages.stride(), v_pages.stride(), table.stride()
+    if ks[3] != 1 or vs[3] != 1 or (ts[1] != 1 and table.shape[1] > 1):
+        raise ValueError("elements of a head and entries of a table row must be adjacent")
+    n, size, Hkv, hd = k_pages.shape
+    B, per = table.shape
+    S3 = ctypes.c_int64 * 3
+    return Pages(k_pages.data_ptr(), v_pages.data_ptr(), S3(*ks[:3]), S3(*vs[:3]), table.data_ptr(),
+                 max(ts[0], per), n, size, per, B, Hkv, hd,
+                 GSRQ_BF16 if k_pages.dtype == torch.bfloat16 else GSRQ_F16)
+
+
+def _heads(x, name, heads, head_dim, rows, dtype, device) -> Heads:
+    if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim or x.shape[0] != rows:
+        raise ValueError(f"{name} must be [{rows}, {heads}, {head_dim}], not {tuple(x.shape)}")
+    if x.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {x.dtype}")
+    if x.device != device:
+        raise ValueError(f"{name} is on {x.device}, expected {device}")
+    s = x.stride()
+    if s[2] != 1:
+        raise ValueError(f"{name}: elements of a head must be adjacent")
+    return Heads(x.data_ptr(), s[0], s[1])
+
+
+def paged_append(k, v, k_pages, v_pages, table, q_start, seq_len, *, q=None, theta=None,
+                 k_norm=None, q_norm=None, eps=1e-6, q_out=None, stream=None):
+    """Put new tokens' keys and values into their pages (see gsrq_paged_append).
+
+    k, v [T, Hkv, head_dim] and q [T, Hq, head_dim] (float32, float16 or
+    bfloat16, any strides); k_pages, v_pages [pages, page_size, Hkv, head_dim]
+    (float16 or bfloat16); table [B, per] int32; q_start [B + 1] and
+    seq_len [B] int32 (seq_len with the new tokens).  theta [head_dim / 2]
+    float64: angle per position, e.g. base ** (-2 * arange(hd / 2) / hd); keys
+    and queries are turned by it.  k_norm, q_norm [head_dim] float32.
+    Returns the queries [T, Hq, head_dim] in the pages' type, or None
+    without q."""
+    torch = _torch()
+    lib = load_library()
+    pages = _pages(k_pages, v_pages, table)
+    dev, hd, B = k_pages.device, pages.head_dim, pages.B
+    T = k.shape[0]
+    dt = _paged_dtype(k, "k")
+    kh = _heads(k, "k", pages.Hkv, hd, T, k.dtype, dev)
+    vh = _heads(v, "v", pages.Hkv, hd, T, k.dtype, dev)
+    Hq = 0
+    if q is not None:
+        Hq = q.shape[1] if q.dim() == 3 else 0
+        qh = _heads(q, "q", Hq, hd, T, k.dtype, dev)
+    elif q_norm is not None or q_out is not None:
+        raise ValueError("q_norm and q_out need q")
+    _need(q_start, "q_start", (torch.int32,), dev, (B + 1,))
+    _need(seq_len, "seq_len", (torch.int32,), dev, (B,))
+    _need(theta, "theta", (torch.float64,), dev, (hd // 2,))
+    _need(k_norm, "k_norm", (torch.float32,), dev, (hd,))
+    _need(q_norm, "q_norm", (torch.float32,), dev, (hd,))
+    _need(q_out, "q_out", (k_pages.dtype,), dev, (T, Hq, hd))
+    with _on(dev, stream):
+        if q is not None and q_out is None:
+            q_out = torch.empty((T, Hq, hd), dtype=k_pages.dtype, device=dev)
+        if T == 0:
+            return q_out
+        st = lib.gsrq_paged_append(
+            ctypes.byref(pages), T, _ptr(q_start), _ptr(seq_len), ctypes.byref(kh), ctypes.byref(vh),
+            None if q is None else ctypes.byref(qh), Hq, dt, _ptr(theta), _ptr(k_norm),
+            _ptr(q_norm), float(eps), _ptr(q_out), _append_stream_handle(stream))
+    if st != GSRQ_OK:
+        _check(st, "gsrq_paged_append")
+    return q_out
+
+
+def paged_restore(k_codes, v_codes, seq_len, k_gain, k_shape, v_gain, v_shape, k_pages, v_pages,
+                  table, *, theta=None, stream=None):
+    """Decode coded contexts into pages (see gsrq_paged_restore): k_codes,
+    v_codes [B, cap, W] packed codes, seq_len [B] int32, codebooks [M, G, K]
+    and [M, G, K, d]; the pages, the table and theta as paged_append takes
+    them."""
+    torch = _torch()
+    lib = load_library()
+    pages = _pages(k_pages, v_pages, table)
+    dev = k_pages.device
+    if k_codes.dim() != 3 or k_shape.dim() != 4:
+        raise ValueError("codes must be [B, cap, W] and codebook shapes [M, G, K, d]")
+    B, cap, W = k_codes.shape
+    M, G, K, d = k_shape.shape
+    if B != pages.B:
+        raise ValueError(f"codes of {B} sequences, a table of {pages.B}")
+    sh = make_shape(max(B * cap, 1), G * d, d, K, M)
+    words = int(lib.gsrq_code_words(ctypes.byref(sh)))
+    if W != words:
+        raise ValueError(f"codes have {W} words a row, expected {words}")
+    for name, t in (("k_codes", k_codes), ("v_codes", v_codes)):
+        _need(t, name, (torch.int32, torch.uint32), dev, (B, cap, W))
+    _need(seq_len, "seq_len", (torch.int32,), dev, (B,))
+    for name, t, size in (("k_gain", k_gain, (M, G, K)), ("k_shape", k_shape, (M, G, K, d)),
+                          ("v_gain", v_gain, (M, G, K)), ("v_shape", v_shape, (M, G, K, d))):
+        _need(t, name, (torch.float32,), dev, size)
+    _need(theta, "theta", (torch.float64,), dev, (pages.head_dim // 2,))
+    if cap == 0:
+        return
+    with _on(dev, stream):
+        st = lib.gsrq_paged_restore(
+            ctypes.byref(pages), ctypes.byref(sh), cap, _ptr(k_codes), _ptr(v_codes),
+            _ptr(seq_len), _ptr(k_gain), _ptr(k_shape), _ptr(v_gain), _ptr(v_shape), _ptr(theta),
+            _append_stream_handle(stream))
+    _check(st, "gsrq_paged_restore")

@@ -1,0 +1,125 @@
+"""What the paged cache's entry points refuse, on the CPU: the C ABI checks its
+arguments before any HIP call (dummy pointers stand for device memory), and
+the binding checks tensors before it calls."""
+import ctypes
+import os
+
+import pytest
+import torch
+
+from paper_2607_01065_amd import gsrq as B
+
+pytestmark = pytest.mark.skipif(not os.path.exists(B.LIB_PATH), reason="libgsrq.so not built")
+
+PTR = 1 << 20
+
+
+def _pages(**kw):
+    base = dict(k=PTR, v=PTR, ks=(16 * 8 * 128, 8 * 128, 128), vs=(16 * 8 * 128, 8 * 128, 128), table=PTR, ldt=4,
+                pages=10, page_size=16, per=4, B=2, Hkv=8, head_dim=128, dtype=B.GSRQ_F16)
+    base.update(kw)
+    S3 = ctypes.c_int64 * 3
+    return B.Pages(base["k"], base["v"], S3(*base["ks"]), S3(*base["vs"]), base["table"], base["ldt"], base["pages"],
+                   base["page_size"], base["per"], base["B"], base["Hkv"], base["head_dim"], base["dtype"])
+
+
+BAD_PAGES = [(dict(k=None), 1), (dict(v=PTR + 8), 1), (dict(table=None), 1), (dict(pages=0), 1), (dict(per=0), 1),
+             (dict(B=0), 1), (dict(Hkv=0), 1), (dict(ldt=3), 1), (dict(dtype=B.GSRQ_F32), 2), (dict(dtype=9), 1),
+             (dict(page_size=24), 2), (dict(page_size=0), 1), (dict(head_dim=96), 2), (dict(head_dim=0), 1),
+             (dict(ks=(16 * 8 * 128, 8 * 128 + 4, 128)), 1), (dict(vs=(0, 8 * 128, 128)), 1),
+             (dict(per=1 << 20, page_size=1 << 12, ldt=1 << 20), 1)]
+
+
+def _append(pages=None, T=5, q_start=PTR, seq_len=PTR, k=PTR, v=PTR, q=PTR, stride=1024, Hq=32, dtype=B.GSRQ_F16,
+            theta=None, k_norm=None, q_norm=None, eps=1e-6, q_out=PTR):
+    lib = B.load_library()
+    heads = [None if x is None else ctypes.byref(B.Heads(x, stride, 128)) for x in (k, v, q)]
+    return lib.gsrq_paged_append(ctypes.byref(pages or _pages()), T, q_start, seq_len, *heads, Hq, dtype, theta, k_norm,
+                                 q_norm, eps, q_out, None)
+
+
+@pytest.mark.parametrize("kw,status", BAD_PAGES)
+def test_append_refuses_pages(kw, status):
+    assert _append(_pages(**kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(T=0), 1), (dict(T=1 << 24), 2), (dict(q_start=None), 1), (dict(seq_len=None), 1), (dict(k=None), 1),
+    (dict(v=PTR + 2), 1), (dict(stride=1028), 1), (dict(Hq=0), 1), (dict(dtype=3), 1), (dict(eps=-1.0), 1),
+    (dict(eps=float("nan")), 1), (dict(q_out=None), 1), (dict(q=None), 1), (dict(q=None, q_out=None, q_norm=PTR), 1),
+    (dict(theta=PTR + 4), 1), (dict(Hq=1 << 17), 2)])
+def test_append_refuses_arguments(kw, status):
+    assert _append(**kw) == status
+
+
+def _restore(pages=None, N=200, D=1024, d=8, K=256, M=1, cap=100, codes=PTR, shape=PTR, seq_len=PTR):
+    lib = B.load_library()
+    sh = B.make_shape(N, D, d, K, M)
+    return lib.gsrq_paged_restore(ctypes.byref(pages or _pages()), ctypes.byref(sh), cap, codes, codes, seq_len, PTR, shape,
+                                  PTR, shape, None, None)
+
+
+@pytest.mark.parametrize("kw,status", BAD_PAGES)
+def test_restore_refuses_pages(kw, status):
+    assert _restore(_pages(**kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(cap=0), 1), (dict(N=199), 1), (dict(D=512), 1), (dict(d=0), 1), (dict(d=4), 2), (dict(d=512), 2), (dict(K=200), 1),
+    (dict(M=0), 1), (dict(codes=None), 1), (dict(shape=PTR + 4), 1), (dict(seq_len=None), 1), (dict(K=1 << 17), 1)])
+def test_restore_refuses_arguments(kw, status):
+    assert _restore(**kw) == status
+
+
+def _tensors(**kw):
+    t = dict(k=torch.zeros((3, 2, 64), dtype=torch.float16), v=torch.zeros((3, 2, 64), dtype=torch.float16),
+             kp=torch.zeros((4, 8, 2, 64), dtype=torch.float16), vp=torch.zeros((4, 8, 2, 64), dtype=torch.float16),
+             table=torch.zeros((2, 2), dtype=torch.int32), q_start=torch.zeros(3, dtype=torch.int32),
+             seq_len=torch.zeros(2, dtype=torch.int32))
+    t.update(kw)
+    return [t[n] for n in ("k", "v", "kp", "vp", "table", "q_start", "seq_len")]
+
+
+@pytest.mark.parametrize("kw,error", [
+    (dict(kp=torch.zeros((4, 8, 64), dtype=torch.float16)), ValueError),
+    (dict(vp=torch.zeros((4, 8, 2, 64), dtype=torch.bfloat16)), TypeError),
+    (dict(kp=torch.zeros((4, 8, 2, 64)), vp=torch.zeros((4, 8, 2, 64))), TypeError),
+    (dict(table=torch.zeros((2, 2), dtype=torch.int64)), TypeError),
+    (dict(table=torch.zeros((2, 4), dtype=torch.int32)[:, ::2]), ValueError),
+    (dict(k=torch.zeros((3, 1, 64), dtype=torch.float16)), ValueError),
+    (dict(v=torch.zeros((2, 2, 64), dtype=torch.float16)), ValueError),
+    (dict(v=torch.zeros((3, 2, 64))), TypeError),
+    (dict(k=torch.zeros((3, 2, 64), dtype=torch.float64)), TypeError),
+    (dict(k=torch.zeros((3, 2, 128), dtype=torch.float16)[..., ::2]), ValueError),
+    (dict(q_start=torch.zeros(2, dtype=torch.int32)), ValueError),
+    (dict(q_start=torch.zeros(3)), TypeError),
+    (dict(seq_len=torch.zeros(3, dtype=torch.int32)), ValueError),
+    (dict(), ValueError),                                # no GPU tensors
+])
+def test_binding_append_refuses(kw, error):
+    with pytest.raises(error):
+        B.paged_append(*_tensors(**kw))
+
+
+def test_binding_append_refuses_options():
+    t = _tensors()
+    for kw, error in ((dict(theta=torch.zeros(32)), TypeError), (dict(theta=torch.zeros(31, dtype=torch.float64)), ValueError),
+                      (dict(q_norm=torch.zeros(64)), ValueError), (dict(k_norm=torch.zeros(32)), ValueError),
+                      (dict(q=torch.zeros((2, 4, 64), dtype=torch.float16)), ValueError),
+                      (dict(q_out=torch.zeros((3, 4, 64), dtype=torch.float16)), ValueError)):
+        with pytest.raises(error):
+            B.paged_append(*t, **kw)
+
+
+def test_binding_restore_refuses():
+    kp = torch.zeros((4, 8, 2, 64), dtype=torch.float16)
+    tab, lens = torch.zeros((2, 2), dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    codes = torch.zeros((2, 5, 4), dtype=torch.int32)
+    gain, shape = torch.zeros((1, 16, 256)), torch.zeros((1, 16, 256, 8))
+    good = dict(k_codes=codes, v_codes=codes, seq_len=lens, k_gain=gain, k_shape=shape, v_gain=gain, v_shape=shape,
+                k_pages=kp, v_pages=kp, table=tab)
+    for kw, error in ((dict(k_codes=codes[:1]), ValueError), (dict(k_codes=codes[..., :3].contiguous()), ValueError),
+                      (dict(v_codes=codes[:, :4]), ValueError), (dict(v_gain=gain[..., :128]), ValueError),
+                      (dict(k_shape=shape[0]), ValueError), (dict(seq_len=lens.long()), TypeError), (dict(), ValueError)):
+        with pytest.raises(error):
+            B.paged_restore(**{**good, **kw})
