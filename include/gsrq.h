@@ -467,6 +467,47 @@ gsrq_status gsrq_paged_append(const gsrq_pages* pages, int64_t T, const int32_t*
                               const double* theta, const float* k_norm, const float* q_norm,
                               float eps, void* q_out, void* stream);
 
+/* One call of attention of new tokens over a paged cache. */
+typedef struct {
+  int64_t T;          /* rows of new tokens, as in gsrq_paged_append        */
+  int32_t Hq;         /* query heads; a multiple of the pages' Hkv          */
+  int32_t window;     /* tokens that a row sees, itself among them; 0: all  */
+  float scale;        /* softmax scale, > 0, normally 1 / sqrt(head_dim)    */
+  uint32_t flags;     /* 0                                                  */
+} gsrq_paged_attn;
+
+/* Workspace bytes gsrq_attn_paged needs (0: none). */
+gsrq_status gsrq_attn_paged_workspace_bytes(const gsrq_paged_attn* s, const gsrq_pages* pages,
+                                            size_t* bytes);
+
+/*
+ * gsrq_attn_paged -- causal attention of every sequence's new tokens over its
+ * pages: one token of a decoding step, drafts of a few, chunks, or whole
+ * prompts, mixed freely.  Rows, q_start, seq_len and positions are those of
+ * gsrq_paged_append, which has put the new tokens' keys and values into the
+ * pages.  Row i at position p and query head h, which reads key/value head
+ * h / (Hq / Hkv), attends to tokens j of its sequence with j <= p,
+ * j > p - window (window > 0) and a page that is there:
+ *   out = sum_j e^(scale q.k_j) v_j / sum_j e^(scale q.k_j)
+ *   lse = ln sum_j e^(scale q.k_j).
+ * A row that sees nothing gets zeros and lse -inf; rows of no sequence are
+ * left as they are.  What lies in tokens that a row does not see (stale
+ * pages, infinities, NaN) does not reach it.
+ *
+ *  q                 [T][Hq][head_dim] rows of the pages' type, turned.
+ *  out               [T][Hq][head_dim] of the pages' type, 16-byte aligned.
+ *  lse               [T][Hq] float32, or NULL.
+ *  workspace         >= gsrq_attn_paged_workspace_bytes(s, pages), 256-byte
+ *                    aligned; nothing is kept in it between calls.
+ * Precision: products of the pages' type with float32 sums; softmax weights
+ * are rounded to the pages' type for the product with the values; maxima,
+ * sums and the joining of pieces are float32.  The result does not depend on
+ * the order in which the GPU runs the work.
+ */
+gsrq_status gsrq_attn_paged(const gsrq_paged_attn* s, const gsrq_pages* pages,
+                            const int32_t* q_start, const int32_t* seq_len, const gsrq_heads* q,
+                            void* out, float* lse, void* workspace, size_t ws_bytes, void* stream);
+
 /*
  * gsrq_paged_restore -- decode a coded context into pages: tokens
  * 0 .. seq_len[b] - 1 of every sequence, values as gsrq_decode gives them and

@@ -7,7 +7,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRCS = [os.path.join(HERE, "csrc", f) for f in ("gsrq.hip", "gsrq_wide.hip", "gsrq_weights.hip", "gsrq_attn.hip",
-                                                  "gsrq_paged.hip")]
+                                                  "gsrq_paged.hip", "gsrq_attn_paged.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libgsrq.so")
 
@@ -26,7 +26,7 @@ def hipcc():
     raise RuntimeError("hipcc not found")
 
 
-# Flags of single translation units.  The attention kernel keeps its MFMA
+# Flags of single translation units.  The attention kernels keep their MFMA
 # accumulators in ordinary VGPRs: with them in AGPRs, the rare rescaling of
 # the output sums (VALU work) made the compiler copy all 64 accumulators to
 # VGPRs on every token block.  The narrow family's block claims are single-
@@ -36,6 +36,7 @@ def hipcc():
 # themselves.
 SRC_FLAGS = {
     "gsrq_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "gsrq_attn_paged.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "gsrq.hip": ["-mllvm", "-amdgpu-atomic-optimizer-strategy=None"],
 }
 

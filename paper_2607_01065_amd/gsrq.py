@@ -55,6 +55,11 @@ class Heads(ctypes.Structure):
                 ("head_stride", ctypes.c_int64)]
 
 
+class PagedAttn(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("Hq", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
 _lib = None
 _vp = ctypes.c_void_p
 
@@ -120,6 +125,11 @@ def load_library(path: str = LIB_PATH):
     lib.gsrq_paged_restore.restype = ctypes.c_int
     lib.gsrq_paged_restore.argtypes = [PP, SP, ctypes.c_int32, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                        _vp, _vp]
+    XP = ctypes.POINTER(PagedAttn)
+    lib.gsrq_attn_paged_workspace_bytes.restype = ctypes.c_int
+    lib.gsrq_attn_paged_workspace_bytes.argtypes = [XP, PP, ctypes.POINTER(ctypes.c_size_t)]
+    lib.gsrq_attn_paged.restype = ctypes.c_int
+    lib.gsrq_attn_paged.argtypes = [XP, PP, _vp, _vp, HP, _vp, _vp, _vp, ctypes.c_size_t, _vp]
     lib.gsrq_timing_enable.restype = ctypes.c_int
     lib.gsrq_timing_enable.argtypes = [ctypes.c_int]
     lib.gsrq_timing_enable_kinds.restype = ctypes.c_int
@@ -652,6 +662,58 @@ def paged_append(k, v, k_pages, v_pages, table, q_start, seq_len, *, q=None, the
     if st != GSRQ_OK:
         _check(st, "gsrq_paged_append")
     return q_out
+
+
+def attn_paged_workspace_bytes(T, Hq, k_pages, v_pages, table, *, window=0) -> int:
+    """Workspace of attn_paged for T rows of Hq query heads over these pages."""
+    n = ctypes.c_size_t()
+    s = PagedAttn(int(T), int(Hq), int(window), 1.0, 0)
+    pages = _pages(k_pages, v_pages, table)
+    _check(load_library().gsrq_attn_paged_workspace_bytes(ctypes.byref(s), ctypes.byref(pages),
+                                                          ctypes.byref(n)),
+           "gsrq_attn_paged_workspace_bytes")
+    return int(n.value)
+
+
+def attn_paged(q, k_pages, v_pages, table, q_start, seq_len, *, scale=None, window=0, lse=False,
+               out=None, workspace=None, stream=None):
+    """Causal attention of new tokens over their sequences' pages (see
+    gsrq_attn_paged), after paged_append of the same rows.  q [T, Hq, head_dim]
+    of the pages' type, any strides.  Returns out [T, Hq, head_dim] of the
+    same type, with lse=True also the rows' log-sum-exp [T, Hq] float32.
+    workspace: a uint8 tensor of attn_paged_workspace_bytes, or None (one is
+    made for the call)."""
+    torch = _torch()
+    lib = load_library()
+    pages = _pages(k_pages, v_pages, table)
+    dev, hd, B = k_pages.device, pages.head_dim, pages.B
+    if q.dim() != 3:
+        raise ValueError("q must be [T, Hq, head_dim]")
+    T, Hq = q.shape[0], q.shape[1]
+    qh = _heads(q, "q", Hq, hd, T, k_pages.dtype, dev)
+    _need(q_start, "q_start", (torch.int32,), dev, (B + 1,))
+    _need(seq_len, "seq_len", (torch.int32,), dev, (B,))
+    _need(out, "out", (q.dtype,), dev, (T, Hq, hd))
+    if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be contiguous, on {dev}")
+    scale = 1.0 / math.sqrt(hd) if scale is None else float(scale)
+    s = PagedAttn(T, Hq, int(window), scale, 0)
+    with _on(dev, stream):
+        if out is None:
+            out = torch.empty((T, Hq, hd), dtype=q.dtype, device=dev)
+        total = torch.empty((T, Hq), dtype=torch.float32, device=dev) if lse else None
+        if T > 0:
+            n = ctypes.c_size_t()
+            _check(lib.gsrq_attn_paged_workspace_bytes(ctypes.byref(s), ctypes.byref(pages),
+                                                       ctypes.byref(n)),
+                   "gsrq_attn_paged_workspace_bytes")
+            ws = _workspace(n.value, dev, workspace) if n.value else None
+            st = lib.gsrq_attn_paged(
+                ctypes.byref(s), ctypes.byref(pages), _ptr(q_start), _ptr(seq_len),
+                ctypes.byref(qh), _ptr(out), _ptr(total), _ptr(ws),
+                0 if ws is None else ws.numel() * ws.element_size(), _append_stream_handle(stream))
+            _check(st, "gsrq_attn_paged")
+    return (out, total) if lse else out
 
 
 def paged_restore(k_codes, v_codes, seq_len, k_gain, k_shape, v_gain, v_shape, k_pages, v_pages,

@@ -123,3 +123,43 @@ def test_binding_restore_refuses():
                       (dict(k_shape=shape[0]), ValueError), (dict(seq_len=lens.long()), TypeError), (dict(), ValueError)):
         with pytest.raises(error):
             B.paged_restore(**{**good, **kw})
+
+
+def _attn(pages=None, T=5, Hq=32, window=0, scale=0.1, flags=0, q_start=PTR, seq_len=PTR, q=PTR, stride=4096, out=PTR,
+          ws=PTR, nbytes=1 << 40):
+    lib = B.load_library()
+    s = B.PagedAttn(T, Hq, window, scale, flags)
+    qh = None if q is None else ctypes.byref(B.Heads(q, stride, 128))
+    return lib.gsrq_attn_paged(ctypes.byref(s), ctypes.byref(pages or _pages()), q_start, seq_len, qh, out, None, ws, nbytes,
+                               None)
+
+
+@pytest.mark.parametrize("kw,status", BAD_PAGES)
+def test_attention_refuses_pages(kw, status):
+    assert _attn(_pages(**kw)) == status
+
+
+LONG = dict(per=1 << 14, ldt=1 << 14)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(T=0), 1), (dict(Hq=0), 1), (dict(Hq=12), 1), (dict(window=-1), 1), (dict(scale=0.0), 1), (dict(scale=-1.0), 1),
+    (dict(scale=float("inf")), 1), (dict(scale=float("nan")), 1), (dict(flags=1), 1), (dict(q_start=None), 1),
+    (dict(seq_len=None), 1), (dict(q=None), 1), (dict(q=PTR + 2), 1), (dict(stride=4100), 1), (dict(out=None), 1),
+    (dict(out=PTR + 8), 1), (dict(pages=_pages(**LONG), ws=None), 1), (dict(pages=_pages(**LONG), ws=PTR + 16), 1),
+    (dict(pages=_pages(**LONG), nbytes=0), 3), (dict(T=1 << 30), 2)])
+def test_attention_refuses_arguments(kw, status):
+    assert _attn(**kw) == status
+
+
+def test_binding_attention_refuses():
+    kp = torch.zeros((4, 8, 2, 64), dtype=torch.float16)
+    tab, lens, start = torch.zeros((2, 2), dtype=torch.int32), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    q = torch.zeros((3, 4, 64), dtype=torch.float16)
+    good = dict(q=q, k_pages=kp, v_pages=kp, table=tab, q_start=start, seq_len=lens)
+    for kw, error in ((dict(q=q.bfloat16()), TypeError), (dict(q=q[0]), ValueError), (dict(q=q[..., :32]), ValueError),
+                      (dict(q_start=start[:2]), ValueError), (dict(seq_len=lens.long()), TypeError),
+                      (dict(out=torch.zeros(3, 4, 64)), TypeError), (dict(out=q[:2]), ValueError),
+                      (dict(workspace=torch.zeros(8, dtype=torch.uint8)[::2]), ValueError), (dict(), ValueError)):
+        with pytest.raises(error):
+            B.attn_paged(**{**good, **kw})
