@@ -4,9 +4,16 @@
 // values j of the pages that the row may see (j <= p, and j > p - window):
 //   o = sum_j softmax_j(scale q . k_j) v_j,   lse = ln sum_j e^(scale q . k_j).
 //
-// The new rows of one sequence and the Hq / Hkv query heads of one key head
-// make one matrix of queries, row r = token * GQ + head, cut into tiles.  Keys
-// and values go through LDS once per tile of queries.  Everything is laid out
+// The new rows of one sequence and the GQ = Hq / Hkv query heads of one key
+// head make one matrix of queries, row r = token * GQ + head.  One launch holds
+// two kinds of workgroups:
+//  * few: a sequence with at most 32 queries per key head (a decoding step, a
+//    few drafts).  Its cost is reading keys and values once, so its keys are
+//    cut into pieces, and each of a workgroup's four waves streams tiles of
+//    32 keys of its own, without a barrier.
+//  * many: 128 queries, 32 a wave; tiles of 64 keys go through LDS for all
+//    four waves.  Keys are cut too where the queries alone do not fill the GPU.
+// A second launch joins the pieces.  In both kinds everything is laid out
 // transposed, so that softmax needs next to no exchange between lanes:
 //  * S^T = K Q^T (v_mfma_f32_32x32x16): A holds 32 keys, B 32 queries, so a
 //    query's scores lie in one lane's registers and its neighbour's 32 lanes
@@ -17,7 +24,8 @@
 // The maximum is a running one, kept until a tile exceeds it by 2^8, and
 // weights are 2^(s - m + 6): at most 2^14, and the float16 subnormals, which
 // lose bits, begin 2^-20 below the maximum.  Weights are rounded to the
-// pages' type (their sum is of the unrounded ones), all sums are float32.
+// pages' type for the product alone (their own sum, which is also a result,
+// is of the unrounded ones); all sums are float32.
 #include <algorithm>
 
 #include "gsrq_paged.h"
@@ -26,7 +34,9 @@ namespace {
 
 constexpr int PT_THREADS = 256;
 constexpr int PT_WAVES = PT_THREADS / 64;
-constexpr int PT_ROWS = 32 * PT_WAVES;     // queries per workgroup
+constexpr int PT_ROWS = 32 * PT_WAVES;     // queries per workgroup of the `many` kind
+constexpr int PT_FEW = 32;                 // queries per key head of the `few` kind, at most
+constexpr int PT_FEW_UNIT = 32 * PT_WAVES; // keys of one round of its four waves
 constexpr float PT_HEADROOM = 8.f;         // log2 by which a tile may exceed the maximum in use
 constexpr float PT_SHIFT = 6.f;            // log2 of the largest weight at a fresh maximum
 
@@ -41,6 +51,7 @@ template <> struct Vec<_Float16> {
   static __device__ __forceinline__ f16v mfma(h8 a, h8 b, f16v c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
+  static constexpr uint32_t EXP = 0x7c007c00u;         // exponent bits of a pair
   static __device__ __forceinline__ h4 read_tr(lds_char* p) {
     typedef __fp16 fp16x4 __attribute__((ext_vector_type(4)));
     return __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4f16(
@@ -53,6 +64,7 @@ template <> struct Vec<__bf16> {
   static __device__ __forceinline__ f16v mfma(b8 a, b8 b, f16v c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
+  static constexpr uint32_t EXP = 0x7f807f80u;
   static __device__ __forceinline__ b4 read_tr(lds_char* p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) b4*)p);
   }
@@ -65,20 +77,17 @@ struct PtArgs {
   void* out;
   float* lse;                     // or null
   const int32_t *q_start, *seq_len;
-  float* part;                    // [row][split][HD] unscaled sums, then [row][split][2]
-  float* part_ml;
-  int T, Hq, GQ, ns, window, slots;
+  // pieces: sums [record][HD] unscaled, [record][2] base and sum of weights;
+  // records of the `few` kind [B][Hkv][32][ns_few], then of the `many` kind
+  // [T][Hq][ns_many]
+  float *part, *part_ml;
+  int64_t many0;                  // first record of the `many` kind
+  int T, Hq, GQ, ns_few, ns_many, window, slots, few_blocks, merge_few;
   float c;                        // scale * log2(e)
 };
 
-// What a tile of queries reads: keys lo .. hi - 1, in `parts` pieces of
-// `step` keys.
-struct Span {
-  int lo, hi, step, parts;
-};
-
-// Sequence b's lengths: new rows [first, first + n), keys [0, keys), and the
-// position of its first new row.
+// Sequence b's new rows [first, first + n), keys [0, keys), and the position
+// of its first new row.
 struct Seq {
   int first, n, keys;
   int64_t pos0;
@@ -94,8 +103,16 @@ __device__ __forceinline__ Seq sequence(const PtArgs& a, int b) {
   return s;
 }
 
-// Queries r0 .. r0 + rows - 1 of a sequence, keys cut at multiples of `unit`
-// into at most ns pieces.
+__device__ __forceinline__ bool is_few(const PtArgs& a, const Seq& s) {
+  return (int64_t)s.n * a.GQ <= PT_FEW;
+}
+
+// What queries r0 .. r0 + rows - 1 of a sequence read: keys lo .. hi - 1, in
+// `parts` pieces of `step` keys, at most ns, cut at multiples of `unit`.
+struct Span {
+  int lo, hi, step, parts;
+};
+
 __device__ __forceinline__ Span span_of(const PtArgs& a, const Seq& s, int r0, int rows, int unit,
                                         int ns) {
   const int64_t most = (int64_t)s.n * a.GQ - 1;
@@ -112,8 +129,8 @@ __device__ __forceinline__ Span span_of(const PtArgs& a, const Seq& s, int r0, i
   return w;
 }
 
-// Tile slot of a launch: sequence b owns the slots from its first row's tile
-// number on, one more than it can need at most.
+// Tile slot of the `many` kind: sequence b owns the slots from its first row's
+// tile number on, one more than it can need at most.
 __device__ __forceinline__ int64_t slot_of(const PtArgs& a, int b) {
   const int q = a.q_start[b];
   return (int64_t)(q < 0 ? 0 : (q > a.T ? a.T : q)) * a.GQ / PT_ROWS + b;
@@ -126,142 +143,174 @@ __device__ __forceinline__ float2 both_halves(float x) {
   return make_float2(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
 
+// The largest of 16 products' sums, NaN left out: fmaxf() would quiet each
+// operand first.  The first maximum is the compiler's own instruction, before
+// which it waits for the matrix unit; for the others, which need its result,
+// it would not.
+__device__ __forceinline__ float max16(f16v x) {
+  float r = __builtin_amdgcn_fmed3f(x[0], x[1], INFINITY);
+  asm("v_max3_f32 %0, %0, %1, %2\n\t"
+      "v_max3_f32 %0, %0, %3, %4\n\t"
+      "v_max3_f32 %0, %0, %5, %6\n\t"
+      "v_max3_f32 %0, %0, %7, %8\n\t"
+      "v_max3_f32 %0, %0, %9, %10\n\t"
+      "v_max3_f32 %0, %0, %11, %12\n\t"
+      "v_max3_f32 %0, %0, %13, %14"
+      : "+v"(r)
+      : "v"(x[2]), "v"(x[3]), "v"(x[4]), "v"(x[5]), "v"(x[6]), "v"(x[7]), "v"(x[8]), "v"(x[9]),
+        "v"(x[10]), "v"(x[11]), "v"(x[12]), "v"(x[13]), "v"(x[14]), "v"(x[15]));
+  return r;
+}
+
 // Places of a tile's 16-byte chunk c of row r in LDS: rows of a key tile are
 // read 32 at a time at one chunk, rows of a value tile four at a time at four
 // chunks, both without bank conflicts in these orders.
+template <int HD> __device__ __forceinline__ int key_chunk(int r, int c) {
+  return c ^ (HD == 64 ? (r >> 1) & 7 : r & 15);
+}
+template <int HD> __device__ __forceinline__ int value_chunk(int r, int c) {
+  return c ^ (4 * (HD == 64 ? (r >> 1) & 1 : r & 3));
+}
 template <int HD> __device__ __forceinline__ int key_at(int r, int c) {
-  return r * (HD * 2) + ((c ^ (HD == 64 ? (r >> 1) & 7 : r & 15)) << 4);
+  return r * (HD * 2) + (key_chunk<HD>(r, c) << 4);
 }
 template <int HD> __device__ __forceinline__ int value_at(int r, int c) {
-  return r * (HD * 2) + ((c ^ (4 * (HD == 64 ? (r >> 1) & 1 : r & 3))) << 4);
+  return r * (HD * 2) + (value_chunk<HD>(r, c) << 4);
 }
 
-template <typename T, int HD> struct PtCfg {
-  static constexpr int TN = HD == 256 ? 32 : 64;       // keys per tile
+template <int HD> struct PtCfg {
+  static constexpr int TN = HD == 256 ? 32 : 64;       // keys per tile of the `many` kind
   static constexpr int CH = HD / 8;                    // 16-byte chunks per row
   static constexpr int BYTES = TN * HD * 2;
   static constexpr int PER = TN * CH / PT_THREADS;     // chunks per thread
+  static constexpr int FEW_BYTES = 32 * HD * 2;        // a wave's tile of the `few` kind
+  static constexpr int FEW_PER = 32 * CH / 64;         // chunks per lane
+  // LDS of a workgroup: two key and two value tiles and which of them held
+  // infinities or NaN, or for `few` a key and a value tile a
+  // wave (where it also joins its waves' sums)
+  static constexpr int FEW_LDS = PT_WAVES * 2 * FEW_BYTES;
+  static constexpr int MANY_LDS = 4 * BYTES + 32;
+  static constexpr int LDS = FEW_LDS > MANY_LDS ? FEW_LDS : MANY_LDS;
 };
 
-// One workgroup per (tile of 128 queries, key head, piece of the keys), 32
-// queries a wave.
-template <typename T, int HD>
-__global__ void __launch_bounds__(PT_THREADS, HD == 256 ? 1 : 2) paged_attn_tile_kernel(PtArgs a) {
-  typedef PtCfg<T, HD> C;
+// 16 bytes a lane from `base` + `offset` (bytes) to LDS, to `to` + 16 * lane;
+// base and `to` the same for the whole wave.  Not waited for: a load that the
+// compiler does not know of, so that it makes no LDS read wait for all loads
+// in flight; wait_loads() does.  Every lane is active at every call (a load
+// that no lane takes part in would be missing in the count of those in flight).
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t to) {
+  asm volatile(
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %0, %1"
+      :
+      : "v"(offset), "s"(base), "s"(to)
+      : "memory", "m0");
+}
+// Until at most N of this wave's loads are in flight.
+template <int N> __device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "i"(N) : "memory");
+}
+// Until this wave's LDS accesses are done.
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
+__device__ __forceinline__ uint32_t lds_offset(const char* p) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const lds_char*)p);
+}
+
+// One wave's queries, as columns: the lane's query, and its part of the sums.
+template <typename T, int HD> struct Columns {
   typedef typename Vec<T>::v8 v8;
   typedef typename Vec<T>::v4 v4;
-  constexpr int NB = C::TN / 32, KS = HD / 16, DT = HD / 32;
-  __shared__ __align__(16) char lds[2 * C::BYTES];
-  char* kt = lds;
-  char* vt = lds + C::BYTES;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int col = lane & 31, half = lane >> 5;
-  const int head = blockIdx.x % a.pool.Hkv;
-  int rest = blockIdx.x / a.pool.Hkv;
-  const int part = rest % a.ns;
-  const int slot = a.slots - 1 - rest / a.ns;          // a prompt's longest rows first
-  int b = 0;
-  for (int i = 0; i < a.pool.B; i += 64) {
-    const bool done = i + lane < a.pool.B && slot_of(a, i + lane + 1) <= slot;
-    b += (int)__popcll(__ballot(done));
-  }
-  b = __builtin_amdgcn_readfirstlane(b);
-  if (b >= a.pool.B) return;
-  const Seq s = sequence(a, b);
-  const int64_t tile = slot - slot_of(a, b);
-  if (tile < 0 || tile * PT_ROWS >= (int64_t)s.n * a.GQ) return;
-  const int r0 = (int)tile * PT_ROWS;
-  const Span w = span_of(a, s, r0, PT_ROWS, C::TN, a.ns);
-  if (part >= w.parts) return;
-  const int begin = w.lo + part * w.step;
-  const int end = min(w.hi, begin + w.step);
+  static constexpr int KS = HD / 16, DT = HD / 32;
+  v8 q[KS];
+  f16v o[DT];
+  float m, l;                     // maximum in use (of scaled scores, log2), sum of weights
+  int see_lo, see_hi;             // keys that the query sees
+  int all_lo, all_hi;             // keys that every query of the wave sees
 
-  // this lane's query
-  const int r = r0 + 32 * wave + col;
-  const bool real = r < s.n * a.GQ;
-  const int tok = real ? r / a.GQ : 0, g = real ? r - tok * a.GQ : 0;
-  const int64_t pos = s.pos0 + tok;
-  const int see_hi = real ? (int)(pos + 1 < s.keys ? (pos + 1 > 0 ? pos + 1 : 0) : s.keys) : 0;
-  const int64_t from = a.window ? pos - a.window + 1 : 0;
-  const int see_lo = from > 0 ? (int)(from < s.keys ? from : s.keys) : 0;
-  v8 qf[KS];
-  {
+  // Query r of the sequence (rows past the last: a copy of row 0 that sees nothing).
+  __device__ __forceinline__ void start(const PtArgs& a, const Seq& s, int head, int r) {
+    const int half = (threadIdx.x >> 5) & 1;
+    const bool real = r < s.n * a.GQ;
+    const int tok = real ? r / a.GQ : 0, g = real ? r - tok * a.GQ : 0;
+    const int64_t pos = s.pos0 + tok;
+    see_hi = real ? (int)(pos + 1 < s.keys ? (pos + 1 > 0 ? pos + 1 : 0) : s.keys) : 0;
+    const int64_t from = a.window ? pos - a.window + 1 : 0;
+    see_lo = from > 0 ? (int)(from < s.keys ? from : s.keys) : 0;
     const T* qp = (const T*)a.q + (int64_t)(s.first + tok) * a.qst[0] +
                   (int64_t)(head * a.GQ + g) * a.qst[1] + 8 * half;
 #pragma unroll
-    for (int k = 0; k < KS; ++k) qf[k] = *(const v8*)(qp + 16 * k);
-  }
-  // keys that every query of the wave sees: no mask between these
-  int all_hi = see_hi, all_lo = see_lo;
+    for (int k = 0; k < KS; ++k) q[k] = *(const v8*)(qp + 16 * k);
+    // (waited for here: the compiler does not count load_to_lds(), and would
+    // wait for those in flight too inside the loop)
 #pragma unroll
-  for (int m = 1; m < 32; m <<= 1) {
-    all_hi = min(all_hi, __shfl_xor(all_hi, m));
-    all_lo = max(all_lo, __shfl_xor(all_lo, m));
-  }
-  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
-
-  f16v o[DT];
+    for (int k = 0; k < KS; ++k) asm volatile("" : "+v"(q[k]));
+    all_hi = see_hi;
+    all_lo = see_lo;
 #pragma unroll
-  for (int t = 0; t < DT; ++t)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-  float m = -INFINITY, l = 0.f;                        // of the scaled scores, log2
-
-  for (int t0 = begin; t0 < end; t0 += C::TN) {
-    // the pages of the tile's tokens, one a lane
-    const int mine = t0 + (lane & (C::TN - 1));
-    const int page = mine < end ? page_of(a.pool, b, mine) : -1;
-    const uint64_t absent = __ballot(page < 0);
-    __syncthreads();                                   // the last tile has been read
-#pragma unroll
-    for (int u = 0; u < C::PER; ++u) {
-      const int i = u * PT_THREADS + tid, row = i / C::CH, ch = i % C::CH;
-      const int pg = __shfl(page, row);
-      u4 kx = {0u, 0u, 0u, 0u}, vx = {0u, 0u, 0u, 0u};
-      if (pg >= 0) {
-        const int64_t in = (t0 + row) & ((1 << a.pool.shift) - 1);
-        kx = *(const u4*)((const T*)a.pool.k + pg * a.pool.ks[0] + in * a.pool.ks[1] +
-                          head * a.pool.ks[2] + 8 * ch);
-        vx = *(const u4*)((const T*)a.pool.v + pg * a.pool.vs[0] + in * a.pool.vs[1] +
-                          head * a.pool.vs[2] + 8 * ch);
-      }
-      *(u4*)(kt + key_at<HD>(row, ch)) = kx;
-      *(u4*)(vt + value_at<HD>(row, ch)) = vx;
+    for (int x = 1; x < 32; x <<= 1) {
+      all_hi = min(all_hi, __shfl_xor(all_hi, x));
+      all_lo = max(all_lo, __shfl_xor(all_lo, x));
     }
-    __syncthreads();
+    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+  }
+
+  // The weights of NB blocks of 32 keys from key t0 on, the keys in LDS.
+  // absent: rows of the tile that nobody sees.
+  template <int NB>
+  __device__ __forceinline__ void weights(const PtArgs& a, const char* kt, int t0, uint64_t absent,
+                                          v8 (&p)[NB][2]) {
+    const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
     f16v sc[NB];
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
+    for (int n = 0; n < NB; ++n)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[n][i] = 0.f;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
         const v8 kf = *(const v8*)(kt + key_at<HD>(32 * n + col, 2 * k + half));
-        sc[n] = Vec<T>::mfma(kf, qf[k], sc[n]);
+        sc[n] = Vec<T>::mfma(kf, q[k], sc[n]);
       }
+    // keys are read four products ahead
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int i = 0; i < KS * NB - 4; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
-    if (absent || t0 + C::TN > all_hi || t0 < all_lo) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    if (absent || t0 + 32 * NB > all_hi || t0 < all_lo) {
+      // (bounds moved to the lane's first row, so that each element compares
+      // with a constant)
+      const int hi = see_hi - t0 - 4 * half, lo = see_lo - t0 - 4 * half;
+      const uint64_t gone = absent >> (4 * half);
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int row = 32 * n + 8 * (i / 4) + 4 * half + i % 4, j = t0 + row;
-          const bool seen = j < see_hi && j >= see_lo && !((absent >> row) & 1);
+          const int row = 32 * n + 8 * (i / 4) + i % 4;
+          const bool seen = row < hi && row >= lo && !((gone >> row) & 1);
           sc[n][i] = seen ? sc[n][i] : -INFINITY;
         }
     }
-    float top = sc[0][0];
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[n][i]);
+    float top = max16(sc[0]);
+    if (NB > 1) top = fmaxf(top, max16(sc[NB - 1]));
     const float2 tops = both_halves(top);
     top = fmaxf(tops.x, tops.y) * a.c;
     if (__any(top > m + PT_HEADROOM)) {
       const float now = fmaxf(m, top);
-      // a query that has seen nothing keeps -inf, and a factor of its own
-      const float f = now == -INFINITY ? 1.f : exp2f(m - now);
+      // (a query that has seen nothing keeps -inf)
+      const float f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
       m = now;
       l *= f;
 #pragma unroll
@@ -273,87 +322,440 @@ __global__ void __launch_bounds__(PT_THREADS, HD == 256 ? 1 : 2) paged_attn_tile
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sc[n][i] = __builtin_amdgcn_exp2f(fmaf(sc[n][i], a.c, sub));
-        l += sc[n][i];
-      }
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(sc[n][8 * k + e], a.c, sub));
+          const float y = __builtin_amdgcn_exp2f(fmaf(sc[n][8 * k + e + 1], a.c, sub));
+          p[n][k][e] = (T)x;
+          p[n][k][e + 1] = (T)y;
+          l += x + y;
+        }
+  }
+
+  // Adds their values, from LDS.
+  template <int NB>
+  __device__ __forceinline__ void add_values(const char* vt, const v8 (&p)[NB][2]) {
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        v8 p;
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = (T)sc[n][8 * k + e];
+        for (int t = 0; t < DT; ++t) o[t] = Vec<T>::mfma(values(vt, n, k, t), p[n][k], o[t]);
+    // values are read two products ahead
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
-        for (int t = 0; t < DT; ++t) {
-          const int row = 32 * n + 16 * k + 4 * half + ((lane & 15) >> 2);
-          const int ch = 4 * t + ((lane >> 3) & 2) + ((lane & 3) >> 1);
-          const v4 lo = Vec<T>::read_tr((lds_char*)(vt + value_at<HD>(row, ch) + 8 * (lane & 1)));
-          const v4 hi = Vec<T>::read_tr((lds_char*)(vt + value_at<HD>(row + 8, ch) + 8 * (lane & 1)));
-          const v8 vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-          o[t] = Vec<T>::mfma(vf, p, o[t]);
-        }
-      }
+    for (int i = 0; i < 2 * NB * DT - 2; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
   }
 
-  const float2 ls = both_halves(l);
-  l = ls.x + ls.y;
-  if (!real) return;
-  const float base = m == -INFINITY ? m : m - PT_SHIFT;
+  // V^T of 32 dimensions and the 16 tokens of weights [n][k], in their order.
+  static __device__ __forceinline__ v8 values(const char* vt, int n, int k, int t) {
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    const int row = 32 * n + 16 * k + 4 * half + ((lane & 15) >> 2);
+    const int ch = 4 * t + ((lane >> 3) & 2) + ((lane & 3) >> 1), in = 8 * (lane & 1);
+    const v4 lo = Vec<T>::read_tr((lds_char*)(vt + value_at<HD>(row, ch) + in));
+    const v4 hi = Vec<T>::read_tr((lds_char*)(vt + value_at<HD>(row + 8, ch) + in));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+
+  // After the last tile: the infinities and NaN that without_infinities() took
+  // out, of `rows` keys every `step` from `from` to `to`, for the queries that
+  // see them.  A weight above zero leaves them what they are, and adding one
+  // twice changes nothing.
+  __device__ __forceinline__ void see_infinities(const PtArgs& a, int b, int head, int from, int to,
+                                                 int step, int rows) {
+    const int half = (threadIdx.x >> 5) & 1;
+    for (int t0 = from; t0 <= to; t0 += step)
+      for (int j = t0; j < t0 + rows; ++j) {
+        const int page = page_of(a.pool, b, j);
+        const bool seen = page >= 0 && j < see_hi && j >= see_lo;
+        if (!__any(seen)) continue;
+        const T* v = (const T*)a.pool.v + page * a.pool.vs[0] +
+                     (int64_t)(j & ((1 << a.pool.shift) - 1)) * a.pool.vs[1] +
+                     head * a.pool.vs[2] + 4 * half;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const v4 x = *(const v4*)(v + 32 * t + 8 * i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float y = (float)x[e];
+              o[t][4 * i + e] += seen && !(fabsf(y) < INFINITY) ? y : 0.f;
+            }
+          }
+      }
+  }
+};
+
+// Takes infinities and NaN out of a 16-byte chunk of values in a tile where
+// some query does not see every row (its weight of zero would make NaN of
+// them); see_infinities() brings them to the queries that see them.  Whether
+// there were any.
+template <typename T> __device__ __forceinline__ bool without_infinities(u4* at) {
+  constexpr uint32_t HI = Vec<T>::EXP & 0xffff0000u, LO = Vec<T>::EXP & 0xffffu;
+  u4 x = *at;
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t w = x[i];
+    if ((w & LO) == LO) w &= 0xffff0000u;
+    if ((w & HI) == HI) w &= 0xffffu;
+    any = any || w != x[i];
+    x[i] = w;
+  }
+  if (any) *at = x;
+  return any;
+}
+
+// First token of a group of rows in one page (pages hold at least 8 tokens, a
+// wave's load takes 64 / CH <= 8 rows): address of one head's keys or values.
+// For an absent page the pool's first tokens, which nobody looks at.
+template <typename T>
+__device__ __forceinline__ const char* rows_of(const PagePool& p, const char* base,
+                                               const int64_t (&st)[3], int page, int t, int head) {
+  const int64_t in = page < 0 ? 0 : t & ((1 << p.shift) - 1);
+  return base + sizeof(T) * ((page < 0 ? 0 : page) * st[0] + in * st[1] + head * st[2]);
+}
+
+// A row's result, from its lane's part of the sums (both halves of l joined).
+template <typename T, int HD>
+__device__ __forceinline__ void put_row(const PtArgs& a, const Columns<T, HD>& c, int64_t orow) {
+  typedef typename Vec<T>::v4 v4;
+  const int half = (threadIdx.x >> 5) & 1;
+  const float inv = c.l == 0.f ? 0.f : 1.f / c.l;
+  T* dst = (T*)a.out + orow * HD + 4 * half;
+#pragma unroll
+  for (int t = 0; t < HD / 32; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (T)(c.o[t][4 * i + e] * inv);
+      *(v4*)(dst + 32 * t + 8 * i) = x;
+    }
+  if (a.lse && half == 0)
+    a.lse[orow] = c.l == 0.f ? -INFINITY
+                             : (c.m - PT_SHIFT + log2f(c.l)) * 0.69314718055994531f;
+}
+
+// 128 queries of one sequence and key head, 32 a wave, and a piece of the keys.
+template <typename T, int HD>
+__device__ __forceinline__ void many(const PtArgs& a, char* lds, int block) {
+  typedef PtCfg<HD> C;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int head = block % a.pool.Hkv;
+  const int rest = block / a.pool.Hkv;
+  const int part = rest % a.ns_many;
+  const int slot = a.slots - 1 - rest / a.ns_many;     // a prompt's longest rows first
+  int b = 0;
+  for (int i = 0; i < a.pool.B; i += 64) {
+    const bool done = i + lane < a.pool.B && slot_of(a, i + lane + 1) <= slot;
+    b += (int)__popcll(__ballot(done));
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  if (b >= a.pool.B) return;
+  const Seq s = sequence(a, b);
+  const int64_t tile = slot - slot_of(a, b);
+  if (is_few(a, s) || tile < 0 || tile * PT_ROWS >= (int64_t)s.n * a.GQ) return;
+  const int r0 = (int)tile * PT_ROWS;
+  const Span w = span_of(a, s, r0, PT_ROWS, C::TN, a.ns_many);
+  if (part >= w.parts) return;
+  const int begin = w.lo + part * w.step;
+  const int end = min(w.hi, begin + w.step);
+  // keys that every query of the workgroup sees
+  const int64_t first = s.pos0 + r0 / a.GQ, last = s.pos0 + (r0 + PT_ROWS - 1) / a.GQ;
+  const bool whole = r0 + PT_ROWS <= s.n * a.GQ;
+  const int wg_hi = whole ? (int)min((int64_t)s.keys, first + 1) : 0;
+  const int64_t wg_lo = a.window ? last - a.window + 1 : 0;
+
+  const int r = r0 + 32 * wave + (lane & 31);
+  Columns<T, HD> c;
+  c.start(a, s, head, r);
+  int* odd_tiles = (int*)(lds + 4 * C::BYTES);         // first and last tile with infinities or NaN
+  if (tid == 0) {
+    odd_tiles[0] = INT32_MAX;
+    odd_tiles[1] = -1;
+  }
+
+  // tile t0 to LDS, pages found one a lane; a wave's load fills 1 KiB
+  constexpr int RL = 64 / C::CH;                       // rows of one load
+  const int lrow = lane / C::CH, lch = lane % C::CH;
+  auto fetch = [&](int t0, int page, const char* kt) {
+#pragma unroll
+    for (int u = 0; u < C::PER; ++u) {
+      const int row = (u * PT_WAVES + wave) * RL;
+      const int pg = __builtin_amdgcn_readlane(page, row);
+      const uint32_t to = lds_offset(kt) + 1024 * (u * PT_WAVES + wave);
+      load_to_lds(rows_of<T>(a.pool, a.pool.k, a.pool.ks, pg, t0 + row, head),
+                  2 * (lrow * (uint32_t)a.pool.ks[1] + 8 * key_chunk<HD>(row + lrow, lch)), to);
+      load_to_lds(rows_of<T>(a.pool, a.pool.v, a.pool.vs, pg, t0 + row, head),
+                  2 * (lrow * (uint32_t)a.pool.vs[1] + 8 * value_chunk<HD>(row + lrow, lch)),
+                  to + C::BYTES);
+    }
+  };
+  const int mine = lane & (C::TN - 1);
+  int entry = entry_of(a.pool, b, begin + mine);
+  int page = begin + mine < end ? checked(a.pool, entry) : -1;
+  uint64_t absent = __ballot(page < 0), next_absent = 0;
+  __syncthreads();                                     // odd_tiles
+  fetch(begin, page, lds);
+  entry = entry_of(a.pool, b, begin + C::TN + mine);
+  int odd = 0;
+  for (int t0 = begin; t0 < end; t0 += C::TN, odd ^= 1, absent = next_absent) {
+    char* kt = lds + odd * 2 * C::BYTES;
+    char* vt = kt + C::BYTES;
+    const bool masked = absent || t0 + C::TN > wg_hi || t0 < wg_lo;
+    wait_loads<0>();
+    if (masked) {
+      // each thread looks at the values that it has loaded; rows of absent
+      // pages become zeros
+      // (opaque: addresses are formed here, not kept in registers)
+      int me = tid;
+      asm volatile("" : "+v"(me));
+#pragma unroll
+      for (int u = 0; u < C::PER; ++u) {
+        const int i = u * PT_THREADS + me, row = i / C::CH;
+        u4* v = (u4*)(vt + 16 * i);
+        if ((absent >> row) & 1) {
+          *v = (u4){0u, 0u, 0u, 0u};
+        } else if (without_infinities<T>(v)) {
+          atomicMin(&odd_tiles[0], t0);
+          atomicMax(&odd_tiles[1], t0);
+        }
+      }
+    }
+    wait_lds();
+    __builtin_amdgcn_s_barrier();                      // tile t0 is there, the other one free
+    asm volatile("" : : : "memory");
+    if (t0 + C::TN < end) {
+      page = t0 + C::TN + mine < end ? checked(a.pool, entry) : -1;
+      next_absent = __ballot(page < 0);
+      fetch(t0 + C::TN, page, lds + (odd ^ 1) * 2 * C::BYTES);
+      entry = entry_of(a.pool, b, t0 + 2 * C::TN + mine);
+    }
+    typename Vec<T>::v8 p[C::TN / 32][2];
+    c.template weights<C::TN / 32>(a, kt, t0, absent, p);
+    c.template add_values<C::TN / 32>(vt, p);
+  }
+  __syncthreads();
+  c.see_infinities(a, b, head, __builtin_amdgcn_readfirstlane(odd_tiles[0]),
+                   __builtin_amdgcn_readfirstlane(odd_tiles[1]), C::TN, C::TN);
+
+  const float2 ls = both_halves(c.l);
+  c.l = ls.x + ls.y;
+  if (r >= s.n * a.GQ) return;
+  const int tok = r / a.GQ, g = r - tok * a.GQ;
   const int64_t orow = (int64_t)(s.first + tok) * a.Hq + head * a.GQ + g;
   if (w.parts == 1) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    T* dst = (T*)a.out + orow * HD + 4 * half;
+    put_row<T, HD>(a, c, orow);
+    return;
+  }
+  const int64_t rec = a.many0 + orow * a.ns_many + part;
+  const int half = lane >> 5;
+  float* dst = a.part + rec * HD + 4 * half;
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
+  for (int t = 0; t < HD / 32; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *(f4*)(dst + 32 * t + 8 * i) =
+          (f4){c.o[t][4 * i], c.o[t][4 * i + 1], c.o[t][4 * i + 2], c.o[t][4 * i + 3]};
+  if (half == 0) *(float2*)(a.part_ml + 2 * rec) = make_float2(c.m, c.l);
+}
+
+// All queries (32 at most) of one sequence and key head, and a piece of the
+// keys: each wave takes every fourth tile of 32 keys, and the waves' sums are
+// joined in LDS.
+template <typename T, int HD>
+__device__ __forceinline__ void few(const PtArgs& a, char* lds, int block) {
+  typedef PtCfg<HD> C;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int head = block % a.pool.Hkv;
+  const int rest = block / a.pool.Hkv;
+  const int part = rest % a.ns_few, b = rest / a.ns_few;
+  const Seq s = sequence(a, b);
+  if (s.n == 0 || !is_few(a, s)) return;
+  const Span w = span_of(a, s, 0, PT_FEW, PT_FEW_UNIT, a.ns_few);
+  if (part >= w.parts) return;
+  const int begin = w.lo + part * w.step + 32 * wave;
+  const int end = min(w.hi, w.lo + (part + 1) * w.step);
+  char* kt = lds + wave * 2 * C::FEW_BYTES;
+  char* vt = kt + C::FEW_BYTES;
+  Columns<T, HD> c;
+  c.start(a, s, head, lane & 31);
+  // keys that every query of the sequence sees
+  const int q_hi = (int)min((int64_t)s.keys, max(s.pos0 + 1, (int64_t)0));
+  const int64_t q_lo = a.window ? s.pos0 + s.n - a.window : 0;
+
+  // the keys or the values of tile t0 to LDS; pages found one a lane
+  constexpr int RL = 64 / C::CH;                       // rows of one load
+  const int lrow = lane / C::CH, lch = lane % C::CH;
+  auto fetch = [&](const char* base, const int64_t (&st)[3], int t0, int page, const char* at,
+                   bool key) {
+    const uint32_t to = lds_offset(at);
+#pragma unroll
+    for (int u = 0; u < C::FEW_PER; ++u) {
+      const int row = u * RL, pg = __builtin_amdgcn_readlane(page, row);
+      const int ch = key ? key_chunk<HD>(row + lrow, lch) : value_chunk<HD>(row + lrow, lch);
+      load_to_lds(rows_of<T>(a.pool, base, st, pg, t0 + row, head),
+                  2 * (lrow * (uint32_t)st[1] + 8 * ch), to + 1024 * u);
+    }
+  };
+  const int mine = lane & 31;
+  auto page_at = [&](int t0, int entry) { return t0 + mine < end ? checked(a.pool, entry) : -1; };
+  int odd_from = INT32_MAX, odd_to = -1;               // tiles with infinities or NaN
+  // Keys and values have one tile's place each: while weights are computed
+  // the values are on their way, and while these are added the next keys.
+  int page = page_at(begin, entry_of(a.pool, b, begin + mine));
+  int next = page_at(begin + PT_FEW_UNIT, entry_of(a.pool, b, begin + PT_FEW_UNIT + mine));
+  if (begin < end) {
+    fetch(a.pool.k, a.pool.ks, begin, page, kt, true);
+    fetch(a.pool.v, a.pool.vs, begin, page, vt, false);
+  }
+  for (int t0 = begin; t0 < end; t0 += PT_FEW_UNIT) {
+    const uint64_t absent = __ballot(page < 0) & 0xffffffffull;
+    wait_loads<C::FEW_PER>();                          // the keys are there
+    const int after = entry_of(a.pool, b, t0 + 2 * PT_FEW_UNIT + mine);
+    typename Vec<T>::v8 p[1][2];
+    c.template weights<1>(a, kt, t0, absent, p);
+    wait_lds();                                        // the keys have been read
+    fetch(a.pool.k, a.pool.ks, t0 + PT_FEW_UNIT, next, kt, true);
+    wait_loads<C::FEW_PER>();                          // the values (and `after`) are there
+    if (absent || t0 + 32 > q_hi || t0 < q_lo) {
+      bool odd = false;
+      int me = lane;
+      asm volatile("" : "+v"(me));
+#pragma unroll
+      for (int u = 0; u < C::FEW_PER; ++u) {
+        u4* v = (u4*)(vt + 16 * (u * 64 + me));
+        if ((absent >> ((u * 64 + me) / C::CH)) & 1) *v = (u4){0u, 0u, 0u, 0u};
+        else odd = without_infinities<T>(v) || odd;
+      }
+      if (__any(odd)) {
+        odd_from = min(odd_from, t0);
+        odd_to = t0;
+      }
+    }
+    c.template add_values<1>(vt, p);
+    wait_lds();                                        // the values have been read
+    fetch(a.pool.v, a.pool.vs, t0 + PT_FEW_UNIT, next, vt, false);
+    page = next;
+    next = page_at(t0 + 2 * PT_FEW_UNIT, after);
+  }
+  wait_loads<0>();                                     // no load writes to LDS from here on
+  c.see_infinities(a, b, head, odd_from, odd_to, PT_FEW_UNIT, 32);
+
+  // join the four waves: [wave][32 queries][HD] sums, in the tiles' LDS
+  const float2 ls = both_halves(c.l);
+  c.l = ls.x + ls.y;
+  __shared__ float ml[PT_WAVES][2][32];
+  const int col = lane & 31, half = lane >> 5;
+  const int rows = s.n * a.GQ;
+  __syncthreads();
+  float* sums = (float*)lds;
+  if (half == 0) {
+    ml[wave][0][col] = c.m;
+    ml[wave][1][col] = c.l;
+  }
+  if (col < rows) {
+#pragma unroll
+    for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        v4 x;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = (T)(o[t][4 * i + e] * inv);
-        *(v4*)(dst + 32 * t + 8 * i) = x;
+        // 16-byte chunks in an order of the row's own against bank conflicts
+        const int ch = (8 * t + 2 * i + half) ^ (col & 7);
+        *(f4*)(sums + (wave * 32 + col) * HD + 4 * ch) =
+            (f4){c.o[t][4 * i], c.o[t][4 * i + 1], c.o[t][4 * i + 2], c.o[t][4 * i + 3]};
       }
-    if (a.lse && half == 0)
-      a.lse[orow] = l == 0.f ? -INFINITY : (base + log2f(l)) * 0.69314718055994531f;
-  } else {
-    float* dst = a.part + (orow * a.ns + part) * HD + 4 * half;
+  }
+  __syncthreads();
+  constexpr int L = HD / 4;                            // lanes per row
+  for (int r = tid / L; r < rows; r += PT_THREADS / L) {
+    float top = ml[0][0][r];
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
+    for (int x = 1; x < PT_WAVES; ++x) top = fmaxf(top, ml[x][0][r]);
+    const int ch = tid % L;
+    f4 o = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *(f4*)(dst + 32 * t + 8 * i) =
-            (f4){o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
-    if (half == 0) {
-      a.part_ml[2 * (orow * a.ns + part)] = base;
-      a.part_ml[2 * (orow * a.ns + part) + 1] = l;
+    for (int x = 0; x < PT_WAVES; ++x) {
+      const float f = ml[x][0][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[x][0][r] - top);
+      const f4 v = *(const f4*)(sums + (x * 32 + r) * HD + 4 * (ch ^ (r & 7)));
+      l += f * ml[x][1][r];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += f * v[e];
+    }
+    if (w.parts == 1) {
+      const int tok = r / a.GQ, g = r - tok * a.GQ;
+      const int64_t orow = (int64_t)(s.first + tok) * a.Hq + head * a.GQ + g;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      typename Vec<T>::v4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (T)(o[e] * inv);
+      *(typename Vec<T>::v4*)((T*)a.out + orow * HD + 4 * ch) = x;
+      if (a.lse && ch == 0)
+        a.lse[orow] = l == 0.f ? -INFINITY : (top - PT_SHIFT + log2f(l)) * 0.69314718055994531f;
+    } else {
+      const int64_t rec =
+          (((int64_t)b * a.pool.Hkv + head) * PT_FEW + r) * a.ns_few + part;
+      *(f4*)(a.part + rec * HD + 4 * ch) = o;
+      if (ch == 0) *(float2*)(a.part_ml + 2 * rec) = make_float2(top, l);
     }
   }
 }
 
-// Joins the pieces of every row whose keys were cut: one wave per (row, head).
+template <typename T, int HD>
+__global__ void __launch_bounds__(PT_THREADS, HD == 256 ? 1 : 2) paged_attn_kernel(PtArgs a) {
+  __shared__ __align__(16) char lds[PtCfg<HD>::LDS];
+  if ((int)blockIdx.x < a.few_blocks) few<T, HD>(a, lds, blockIdx.x);
+  else many<T, HD>(a, lds, blockIdx.x - a.few_blocks);
+}
+
+// Joins the pieces of every row whose keys were cut: one wave per row and head.
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
   constexpr int E = HD / 64;
-  const int64_t orow = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
-  if (orow >= (int64_t)a.T * a.Hq) return;
-  const int row = (int)(orow / a.Hq), head = (int)(orow % a.Hq);
-  const int b = sequence_of(a.q_start, a.pool.B, row);
-  if (b < 0) return;
-  const Seq s = sequence(a, b);
-  const int r = (row - s.first) * a.GQ + head % a.GQ;
-  const Span w = span_of(a, s, r / PT_ROWS * PT_ROWS, PT_ROWS, PtCfg<T, HD>::TN, a.ns);
-  if (w.parts < 2) return;
-  const float* ml = a.part_ml + 2 * orow * a.ns;
+  int64_t rec, orow;
+  int parts;
+  if ((int)blockIdx.x < a.merge_few) {
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int r = i % PT_FEW, head = i / PT_FEW % a.pool.Hkv, b = i / PT_FEW / a.pool.Hkv;
+    const Seq s = sequence(a, b);
+    if (!is_few(a, s) || r >= s.n * a.GQ) return;
+    parts = span_of(a, s, 0, PT_FEW, PT_FEW_UNIT, a.ns_few).parts;
+    rec = (int64_t)i * a.ns_few;
+    const int tok = r / a.GQ;
+    orow = (int64_t)(s.first + tok) * a.Hq + head * a.GQ + r - tok * a.GQ;
+  } else {
+    orow = ((int64_t)blockIdx.x - a.merge_few) * 4 + (threadIdx.x >> 6);
+    if (orow >= (int64_t)a.T * a.Hq) return;
+    const int row = (int)(orow / a.Hq), head = (int)(orow % a.Hq);
+    const int b = sequence_of(a.q_start, a.pool.B, row);
+    if (b < 0) return;
+    const Seq s = sequence(a, b);
+    if (is_few(a, s)) return;
+    const int r = (row - s.first) * a.GQ + head % a.GQ;
+    parts = span_of(a, s, r / PT_ROWS * PT_ROWS, PT_ROWS, PtCfg<HD>::TN, a.ns_many).parts;
+    rec = a.many0 + orow * a.ns_many;
+  }
+  if (parts < 2) return;
+  const float2* ml = (const float2*)a.part_ml + rec;
   float top = -INFINITY;
-  for (int i = 0; i < w.parts; ++i) top = fmaxf(top, ml[2 * i]);
+  for (int i = 0; i < parts; ++i) top = fmaxf(top, ml[i].x);
   float l = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-  for (int i = 0; i < w.parts; ++i) {
-    const float f = ml[2 * i] == -INFINITY ? 0.f : exp2f(ml[2 * i] - top);
-    const float* p = a.part + (orow * a.ns + i) * HD + lane * E;
-    l += f * ml[2 * i + 1];
+  for (int i = 0; i < parts; ++i) {
+    const float f = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[i].x - top);
+    const float* p = a.part + (rec + i) * HD + lane * E;
+    l += f * ml[i].y;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] += f * p[e];
   }
@@ -361,15 +763,15 @@ __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
 #pragma unroll
   for (int e = 0; e < E; ++e) ((T*)a.out)[orow * HD + lane * E + e] = (T)(o[e] * inv);
   if (a.lse && lane == 0)
-    a.lse[orow] = l == 0.f ? -INFINITY : (top + log2f(l)) * 0.69314718055994531f;
+    a.lse[orow] = l == 0.f ? -INFINITY : (top - PT_SHIFT + log2f(l)) * 0.69314718055994531f;
 }
 
 // --------------------------------------------------------------- host side
 
 struct PtPlan {
   PagePool pool;
-  int64_t slots;
-  int ns;
+  int64_t slots, many0;
+  int ns_few, ns_many, few_blocks, many_blocks, merge_few, merge_many;
   size_t off_ml, bytes;
 };
 
@@ -381,27 +783,44 @@ gsrq_status pt_plan(const gsrq_paged_attn* s, const gsrq_pages* pages, PtPlan& p
   if (!(s->scale > 0.f) || !(s->scale < INFINITY)) return GSRQ_E_ARG;
   const int64_t GQ = s->Hq / pages->Hkv;
   if (s->T * GQ > INT32_MAX / 2 || pages->B > (1 << 20)) return GSRQ_E_UNSUPPORTED;
-  p.slots = s->T * GQ / PT_ROWS + pages->B;
-  // keys are cut until the launch has two workgroups per CU, into pieces of
-  // 512 at the least
-  const int64_t wgs = p.slots * pages->Hkv, cap = (int64_t)pages->per * pages->page_size;
-  int64_t ns = std::min<int64_t>((512 + wgs - 1) / wgs, (cap + 511) / 512);
-  if (ns < 1) ns = 1;
-  p.ns = (int)ns;
-  if (wgs * ns > MAX_BLOCKS || (s->T * s->Hq + 3) / 4 > MAX_BLOCKS) return GSRQ_E_UNSUPPORTED;
-  const size_t rows = ns > 1 ? (size_t)(s->T * s->Hq * ns) : 0;
+  const int64_t Hkv = pages->Hkv, B = pages->B, cap = (int64_t)pages->per * pages->page_size;
+  // `few`: pieces for four rounds of two workgroups per CU (lengths differ),
+  // of one round of the four waves at the least
+  const int64_t few = std::max<int64_t>(
+      1, std::min((1024 + B * Hkv - 1) / (B * Hkv), (cap + PT_FEW_UNIT - 1) / PT_FEW_UNIT));
+  // `many`: none where no sequence can have more than 32 queries; cut until
+  // the launch has two workgroups per CU, into pieces of 512 keys at the least
+  p.slots = s->T * GQ > PT_FEW ? s->T * GQ / PT_ROWS + B : 0;
+  int64_t many = 1;
+  if (p.slots)
+    many = std::max<int64_t>(
+        1, std::min((512 + p.slots * Hkv - 1) / (p.slots * Hkv), (cap + 511) / 512));
+  const int64_t few_blocks = B * Hkv * few, many_blocks = p.slots * Hkv * many;
+  const int64_t merge_few = few > 1 ? B * Hkv * (PT_FEW / 4) : 0;
+  const int64_t merge_many = p.slots && many > 1 ? (s->T * s->Hq + 3) / 4 : 0;
+  if (few_blocks + many_blocks > MAX_BLOCKS || merge_few + merge_many > MAX_BLOCKS)
+    return GSRQ_E_UNSUPPORTED;
+  p.ns_few = (int)few;
+  p.ns_many = (int)many;
+  p.few_blocks = (int)few_blocks;
+  p.many_blocks = (int)many_blocks;
+  p.merge_few = (int)merge_few;
+  p.merge_many = (int)merge_many;
+  p.many0 = few > 1 ? B * Hkv * PT_FEW * few : 0;
+  const size_t rows = (size_t)p.many0 + (merge_many ? (size_t)(s->T * s->Hq * many) : 0);
   p.off_ml = align256(rows * pages->head_dim * sizeof(float));
   p.bytes = p.off_ml + align256(rows * 2 * sizeof(float));
   return GSRQ_OK;
 }
 
-template <typename T, int HD> gsrq_status pt_launch(const PtArgs& a, hipStream_t st) {
+template <typename T, int HD>
+gsrq_status pt_launch(const PtArgs& a, const PtPlan& p, hipStream_t st) {
+  static_assert(PtCfg<HD>::LDS <= 160 * 1024 - 2048, "LDS of a CU");
   TimedLaunch tl(GSRQ_KERNEL_ATTENTION, st);
-  const unsigned blocks = (unsigned)a.slots * a.ns * a.pool.Hkv;
-  paged_attn_tile_kernel<T, HD><<<blocks, PT_THREADS, 0, st>>>(a);
+  paged_attn_kernel<T, HD><<<p.few_blocks + p.many_blocks, PT_THREADS, 0, st>>>(a);
   gsrq_status e = launch_ok();
-  if (e || a.ns == 1) return e;
-  paged_attn_merge_kernel<T, HD><<<(unsigned)(((int64_t)a.T * a.Hq + 3) / 4), 256, 0, st>>>(a);
+  if (e || p.merge_few + p.merge_many == 0) return e;
+  paged_attn_merge_kernel<T, HD><<<p.merge_few + p.merge_many, 256, 0, st>>>(a);
   return launch_ok();
 }
 
@@ -443,20 +862,24 @@ gsrq_status gsrq_attn_paged(const gsrq_paged_attn* s, const gsrq_pages* pages,
   a.T = (int)s->T;
   a.Hq = s->Hq;
   a.GQ = s->Hq / pages->Hkv;
-  a.ns = p.ns;
+  a.ns_few = p.ns_few;
+  a.ns_many = p.ns_many;
+  a.few_blocks = p.few_blocks;
+  a.merge_few = p.merge_few;
+  a.many0 = p.many0;
   a.window = s->window;
   a.slots = (int)p.slots;
   a.c = (float)((double)s->scale * 1.4426950408889634);
   hipStream_t st = (hipStream_t)stream;
   const int hd = pages->head_dim;
   if (pages->dtype == GSRQ_F16) {
-    if (hd == 64) return pt_launch<_Float16, 64>(a, st);
-    if (hd == 128) return pt_launch<_Float16, 128>(a, st);
-    return pt_launch<_Float16, 256>(a, st);
+    if (hd == 64) return pt_launch<_Float16, 64>(a, p, st);
+    if (hd == 128) return pt_launch<_Float16, 128>(a, p, st);
+    return pt_launch<_Float16, 256>(a, p, st);
   }
-  if (hd == 64) return pt_launch<__bf16, 64>(a, st);
-  if (hd == 128) return pt_launch<__bf16, 128>(a, st);
-  return pt_launch<__bf16, 256>(a, st);
+  if (hd == 64) return pt_launch<__bf16, 64>(a, p, st);
+  if (hd == 128) return pt_launch<__bf16, 128>(a, p, st);
+  return pt_launch<__bf16, 256>(a, p, st);
 }
 
 }  // extern "C"

@@ -32,9 +32,10 @@ inline gsrq_status page_pool(const gsrq_pages* p, PagePool& o) {
   if (p->ldt < p->per || p->head_dim < 1) return GSRQ_E_ARG;
   if (p->dtype != GSRQ_F16 && p->dtype != GSRQ_BF16)
     return p->dtype == GSRQ_F32 ? GSRQ_E_UNSUPPORTED : GSRQ_E_ARG;
-  if ((int64_t)p->page_size * p->per > INT32_MAX) return GSRQ_E_ARG;
+  if ((int64_t)p->page_size * p->per > (1 << 30)) return GSRQ_E_ARG;
   if (p->head_dim != 64 && p->head_dim != 128 && p->head_dim != 256) return GSRQ_E_UNSUPPORTED;
-  if (!is_pow2(p->page_size)) return GSRQ_E_UNSUPPORTED;
+  if (!is_pow2(p->page_size) || p->page_size < 8) return GSRQ_E_UNSUPPORTED;
+  if (p->k_stride[1] >= 1 << 26 || p->v_stride[1] >= 1 << 26) return GSRQ_E_UNSUPPORTED;
   if ((uintptr_t)p->k % 16 || (uintptr_t)p->v % 16) return GSRQ_E_ARG;
   const int count[3] = {p->pages, p->page_size, p->Hkv};
   for (int i = 0; i < 3; ++i) {
@@ -70,6 +71,16 @@ __device__ __forceinline__ int page_of(const PagePool& p, int b, int64_t pos) {
   if (pos < 0 || (pos >> p.shift) >= p.per) return -1;
   const int page = p.table[b * p.ldt + (pos >> p.shift)];
   return page >= 0 && page < p.pages ? page : -1;
+}
+
+// The table's entry for a position >= 0 (past the row's end: its last), to be
+// looked at only by checked(): a load that nothing waits for yet.
+__device__ __forceinline__ int entry_of(const PagePool& p, int b, int pos) {
+  const int i = pos >> p.shift;
+  return p.table[b * p.ldt + (i < p.per ? i : p.per - 1)];
+}
+__device__ __forceinline__ int checked(const PagePool& p, int entry) {
+  return entry >= 0 && entry < p.pages ? entry : -1;
 }
 
 // First new row and number of new rows of sequence b, held inside [0, T).

@@ -65,14 +65,14 @@ def _check(c, window=0, scale=None, **kw):
 
 
 @pytest.mark.parametrize("counts,lens,Hq,Hkv,hd,page,dtype,window,gap,order", [
-    ([1], [1], 1, 1, 64, 1, "f16", 0, 0, "token"),
+    ([1], [1], 1, 1, 64, 8, "f16", 0, 0, "token"),
     ([1], [1], 4, 1, 128, 16, "bf16", 0, 2, "token"),
     ([1], [63], 4, 1, 128, 16, "f16", 0, 0, "token"),
     ([1], [701], 32, 8, 128, 16, "f16", 0, 0, "token"),
     ([1, 1, 0, 1, 1], [64, 65, 7, 200, 1], 8, 2, 128, 16, "f16", 0, 0, "head"),
     ([1, 1], [3000, 17], 16, 1, 64, 32, "bf16", 0, 0, "token"),
     ([1, 1], [900, 333], 14, 2, 256, 8, "f16", 0, 0, "token"),
-    ([5, 3, 9], [400, 3, 10], 6, 2, 128, 2, "bf16", 0, 1, "token"),            # drafts, pages of two
+    ([5, 3, 9], [400, 3, 10], 6, 2, 128, 8, "bf16", 0, 1, "token"),            # drafts
     ([40], [40], 4, 4, 64, 64, "f16", 0, 0, "head"),                           # a prompt
     ([200, 129], [200, 1029], 8, 2, 128, 16, "f16", 0, 0, "token"),
     ([130], [600], 3, 1, 256, 128, "bf16", 0, 0, "token"),
@@ -111,6 +111,24 @@ def test_absent_pages_and_stale_places():
     c["tab"][0, 3], c["tab"][1, 0], c["tab"][2, 7] = -1, 10 ** 6, -7
     _stale(c)
     _check(c)
+
+
+@pytest.mark.parametrize("window", [0, 40])
+@pytest.mark.parametrize("counts,lens,hd,dtype", [([3, 1], [50, 40], 128, "f16"), ([170, 5], [300, 70], 128, "bf16"),
+                                                  ([100], [100], 64, "f16"), ([90, 2], [200, 99], 256, "bf16")])
+def test_infinities_reach_only_the_rows_that_see_them(counts, lens, hd, dtype, window):
+    """Infinities and NaN in values and keys of tokens in the middle of a chunk: rows before them (and, with a window,
+    rows far behind) stay what they were, rows that see them get what the definition gives."""
+    c = _case(counts, lens, 4, 2, hd, 16, dtype)
+    page = 16
+    bad = [float("nan"), float("inf"), -float("inf")]
+    for b, L in enumerate(lens):
+        for i, t in enumerate((L - 1, L - 2, L - counts[b] // 2 - 1, L // 3)):
+            at = int(c["tab"][b, t // page])
+            c["vp"][at, t % page, i % 2, (7 * i + b) % hd] = bad[i % 3]
+            if i == 1:
+                c["kp"][at, t % page, 1, 3] = bad[0]
+    _check(c, window)
 
 
 def _stale(c):

@@ -55,7 +55,7 @@ def _inputs(counts, Hq, Hkv, hd, dtype, gap=0, seed=0):
 
 
 @pytest.mark.parametrize("src,held,counts,lens,Hq,Hkv,hd,page,order,rope,norm,gap", [
-    ("f16", "f16", [1], [1], 1, 1, 64, 1, "token", True, False, 0),                    # one token, pages of one
+    ("f16", "f16", [1], [1], 1, 1, 64, 8, "token", True, False, 0),                    # one token
     ("f16", "f16", [1] * 9, [1, 2, 15, 16, 17, 31, 100, 64, 65], 32, 8, 128, 16, "token", True, False, 0),
     ("bf16", "bf16", [5, 0, 33, 1], [70, 9, 33, 128], 12, 4, 128, 32, "head", True, True, 3),   # rows behind the last
     ("f32", "f16", [7, 40], [7, 41], 16, 16, 64, 8, "token", False, False, 0),
@@ -112,8 +112,8 @@ def test_append_far_positions_and_strided_rows():
 def test_append_leaves_out_what_has_no_place():
     """Absent pages, positions before the first and behind the last: nothing is written for them, the queries
     are turned all the same."""
-    Hq, Hkv, hd, page = 2, 2, 64, 4
-    counts, lens = [6, 6, 6], [3, 20, 12]               # before the first; behind the table's 16; a hole
+    Hq, Hkv, hd, page = 2, 2, 64, 8
+    counts, lens = [6, 6, 12], [3, 36, 24]              # before the first; behind the table's 32; a hole
     start, k, v, q, _ = _inputs(counts, Hq, Hkv, hd, torch.float16)
     tab = torch.tensor([[0, 1, 2, 3], [4, 5, 6, 7], [8, -1, 99, 10]], dtype=torch.int32)
     kp, vp = (R.pool(12, page, Hkv, hd, torch.float16, "token", s) for s in (1, 2))
@@ -125,7 +125,7 @@ def test_append_leaves_out_what_has_no_place():
                          theta=theta.cuda())
     _close(got, qd, qm, "q")
     touched = km.abs().sum((-1, -2)) > 0
-    assert int(touched.sum()) == 3 + 2                  # of 18 tokens
+    assert int(touched.sum()) == 3 + 2                  # of 24 tokens
     assert torch.equal(kc.cpu()[~touched], kp[~touched]) and torch.equal(vc.cpu()[~touched], vp[~touched])
     _close(kc, kd, km, "k")
     _close(vc, vd, vm, "v")
@@ -160,14 +160,14 @@ def _books(M, G, K, d, seed):
 
 
 @pytest.mark.parametrize("lens,cap,Hkv,hd,d,K,M,page,held,rope", [
-    ([1], 1, 1, 64, 8, 256, 1, 1, "f16", True),
+    ([1], 1, 1, 64, 8, 256, 1, 8, "f16", True),
     ([77, 0, 130], 130, 8, 128, 8, 256, 1, 16, "f16", True),        # the 1-bit layout, one sequence empty
     ([40, 100], 90, 2, 128, 128, 256, 12, 8, "bf16", True),         # 0.75 bit; a length past the codes
     ([33], 40, 3, 128, 16, 256, 4, 64, "f16", False),
     ([50, 51], 60, 2, 64, 64, 64, 3, 16, "bf16", True),             # 6-bit codes, across words
     ([20], 20, 4, 128, 256, 4096, 2, 32, "f16", True),              # a codeword over two heads, 12-bit codes
     ([70, 65], 70, 2, 256, 8, 256, 2, 16, "bf16", True),
-    ([25], 30, 2, 256, 32, 2, 5, 4, "f16", True),
+    ([25], 30, 2, 256, 32, 2, 5, 8, "f16", True),
 ])
 def test_restore(lens, cap, Hkv, hd, d, K, M, page, held, rope):
     """Codes of both sides into pages.  Tolerance: half a step of the type, the rotation as above (its 9 roundings
