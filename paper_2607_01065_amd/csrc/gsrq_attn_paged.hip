@@ -746,18 +746,34 @@ __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
     rec = a.many0 + orow * a.ns_many;
   }
   if (parts < 2) return;
-  const float2* ml = (const float2*)a.part_ml + rec;
-  float top = -INFINITY;
-  for (int i = 0; i < parts; ++i) top = fmaxf(top, ml[i].x);
-  float l = 0.f, o[E];
+  // 64 pieces at a time, one a lane; then their sums, eight loads in flight
+  float top = -INFINITY, l = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-  for (int i = 0; i < parts; ++i) {
-    const float f = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[i].x - top);
-    const float* p = a.part + (rec + i) * HD + lane * E;
-    l += f * ml[i].y;
+  for (int i0 = 0; i0 < parts; i0 += 64) {
+    const int count = min(64, parts - i0);
+    const float2 ml = lane < count ? ((const float2*)a.part_ml)[rec + i0 + lane]
+                                   : make_float2(-INFINITY, 0.f);
+    float now = ml.x;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] += f * p[e];
+    for (int x = 1; x < 64; x <<= 1) now = fmaxf(now, __shfl_xor(now, x));
+    now = fmaxf(now, top);
+    const float old = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now);
+    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - now);
+    float sum = f * ml.y;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
+    top = now;
+    l = l * old + sum;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= old;
+    const float* p = a.part + (rec + i0) * HD + lane * E;
+#pragma unroll 8
+    for (int i = 0; i < count; ++i) {
+      const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] += fi * p[(int64_t)i * HD + e];
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll

@@ -79,6 +79,9 @@ __device__ __forceinline__ int entry_of(const PagePool& p, int b, int pos) {
   const int i = pos >> p.shift;
   return p.table[b * p.ldt + (i < p.per ? i : p.per - 1)];
 }
+__device__ __forceinline__ bool in_table(const PagePool& p, int pos) {
+  return (pos >> p.shift) < p.per;
+}
 __device__ __forceinline__ int checked(const PagePool& p, int entry) {
   return entry >= 0 && entry < p.pages ? entry : -1;
 }

@@ -9,7 +9,11 @@
 // so a rotation needs no exchange and every access is 16 bytes (float32: 32).
 //
 // Restoring.  A token's row is the sum of its stages' codewords fl32(g s),
-// keys then turned in float32 at the token's position.
+// keys then turned in float32 at the token's position.  A workgroup owns 64
+// dimensions of one head, 32 and the 32 they are turned with, of the keys or
+// of the values: a stage's codewords there are K rows of 256 bytes in LDS.
+#include <algorithm>
+
 #include "gsrq_paged.h"
 
 namespace {
@@ -172,7 +176,271 @@ __device__ __forceinline__ void codeword_sum(const RestoreArgs& a, const uint32_
   }
 }
 
-// A lane per 16 elements of a head of one token's key or value row.
+// One workgroup's share of a restored cache: 64 dimensions of one head's keys
+// or values.  The slices of one head's codewords stay on one XCD.
+struct Slice {
+  const uint32_t* codes;
+  const float *gain, *shape;
+  char* base;
+  int64_t st0, st1;               // page, token (bytes)
+  bool turn;
+  int lo, hi;                     // first elements of the halves in a row of D
+  int first;                      // of the lower half in the head
+};
+
+template <typename TP>
+__device__ __forceinline__ Slice slice_of(const RestoreArgs& a, int sub) {
+  const int slices = a.hd / 64;
+  const bool key = !(sub & 1);
+  const int slice = (sub >> 1) % slices, head = (sub >> 1) / slices;
+  const int64_t* st = key ? a.pool.ks : a.pool.vs;
+  Slice s;
+  s.codes = key ? a.k_codes : a.v_codes;
+  s.gain = key ? a.k_gain : a.v_gain;
+  s.shape = key ? a.k_shape : a.v_shape;
+  s.first = 32 * slice;
+  s.base = (key ? a.pool.k : a.pool.v) + (head * st[2] + s.first) * (int64_t)sizeof(TP);
+  s.st0 = st[0] * (int64_t)sizeof(TP);
+  s.st1 = st[1] * (int64_t)sizeof(TP);
+  s.turn = key && a.theta;
+  s.lo = head * a.hd + s.first;
+  s.hi = s.lo + a.hd / 2;
+  return s;
+}
+
+// Four elements from element e on of codeword k of a stage, rounded to float32
+// before any sum.
+__device__ __forceinline__ f4 codeword4(const RestoreArgs& a, const Slice& s, int m, int k, int e) {
+#pragma clang fp contract(off)
+  const int g = e / a.d;
+  const int64_t cb = ((int64_t)m * a.G + g) * a.K + k;
+  const f4 v = *(const f4*)(s.shape + cb * a.d + (e - g * a.d));
+  const float gk = s.gain[cb];
+  return (f4){gk * v[0], gk * v[1], gk * v[2], gk * v[3]};
+}
+
+// Where a token's slice goes; null: its page is not there.
+__device__ __forceinline__ char* token_at(const RestoreArgs& a, const Slice& s, int page, int t) {
+  return page < 0 ? nullptr
+                  : s.base + page * s.st0 + (t & ((1 << a.pool.shift) - 1)) * s.st1;
+}
+
+// All stages' codewords of the slice in LDS (M K 256 bytes), kept while the
+// workgroup goes through chunks of the tokens, its own of the launch's
+// `ranges`.  Four lanes share a token, each with 8 dimensions of the lower half
+// and the 8 they are turned with: two codes and four 16-byte gathers a stage.
+// The 16 columns of an LDS row are permuted by the codeword's index, so that
+// four tokens' gathers, which all want the same columns, meet in a bank twice
+// and not four times.  Angles: position = chunk + 128 slot + row; the row's
+// rotation stays in registers, the chunk's slots' go through LDS, so that a
+// sine is computed per 128 tokens; c and s carry 15 roundings.
+// Bound by its stores (4 x 32768 tokens x 1024, 1 bit: 0.43 GB).
+constexpr int PR_THREADS = 512;
+constexpr int PR_ROWS = PR_THREADS / 4;
+constexpr int PR_SLOTS = 4;
+constexpr int PR_CHUNK = PR_ROWS * PR_SLOTS;
+constexpr int PR_TABLE = 128 * 1024;        // bytes of codewords, at most
+
+template <typename TP>
+__global__ void __launch_bounds__(PR_THREADS, 4) paged_decode_lds_kernel(RestoreArgs a, int nsub,
+                                                                         int ranges) {
+  extern __shared__ __align__(16) f4 tab[];                 // [M][K][16]
+  __shared__ float2 turns[2][PR_SLOTS][32];
+  const int tid = threadIdx.x, l = tid & 3, rg = tid >> 2;
+  const Slice s = slice_of<TP>(a, blockIdx.x % nsub);
+  const int lo = s.lo + 8 * l, hi = s.hi + 8 * l;
+  for (int i = tid; i < a.M * a.K * 16; i += PR_THREADS) {
+    const int m = i / 16 / a.K, k = i / 16 - m * a.K, c = i & 15;
+    const int q = (c >> 2) ^ (k & 3);                       // lower 0, 1, upper 2, 3
+    tab[i] = codeword4(a, s, m, k, (q < 2 ? s.lo : s.hi) + 8 * (c & 3) + 4 * (q & 1));
+  }
+  float cr[8], sr[8];
+  if (s.turn) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) turn_of(rg, a.theta[s.first + 8 * l + j], cr[j], sr[j]);
+  }
+  __syncthreads();
+  const int per = (a.cap + PR_CHUNK - 1) / PR_CHUNK;
+  int buf = 0;
+  for (int64_t c = blockIdx.x / nsub; c < (int64_t)per * a.pool.B; c += ranges) {
+    const int b = (int)(c / per), t0 = (int)(c - (int64_t)b * per) * PR_CHUNK;
+    const int len = min(a.seq_len[b], a.cap);
+    if (t0 >= len) continue;
+    if (s.turn) {
+      if (tid < 32 * PR_SLOTS) {
+        float2 x;
+        turn_of(t0 + PR_ROWS * (tid >> 5), a.theta[s.first + (tid & 31)], x.x, x.y);
+        turns[buf][tid >> 5][tid & 31] = x;
+      }
+      __syncthreads();
+    }
+    int entry[PR_SLOTS];
+#pragma unroll
+    for (int u = 0; u < PR_SLOTS; ++u)
+      entry[u] = entry_of(a.pool, b, min(t0 + PR_ROWS * u + rg, len - 1));
+    const uint32_t* rows = s.codes + ((int64_t)b * a.cap + t0) * a.words;
+#pragma unroll
+    for (int u = 0; u < PR_SLOTS; ++u) {
+      const int t = t0 + PR_ROWS * u + rg;
+      const uint32_t* row = rows + (int64_t)min(PR_ROWS * u + rg, len - 1 - t0) * a.words;
+      float x[8], y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = y[j] = 0.f;
+      for (int m = 0; m < a.M; ++m) {
+        const int kx = code_at(row, ((int64_t)m * a.G + lo / a.d) * a.b, a.b);
+        const int ky = code_at(row, ((int64_t)m * a.G + hi / a.d) * a.b, a.b);
+        const f4* tx = tab + (m * a.K + kx) * 16 + l;
+        const f4* ty = tab + (m * a.K + ky) * 16 + l;
+        const f4 x0 = tx[4 * (kx & 3)], x1 = tx[4 * ((kx & 3) ^ 1)];
+        const f4 y0 = ty[4 * ((ky & 3) ^ 2)], y1 = ty[4 * ((ky & 3) ^ 3)];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[j] += x0[j];
+          x[4 + j] += x1[j];
+          y[j] += y0[j];
+          y[4 + j] += y1[j];
+        }
+      }
+      if (s.turn) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float2 w = turns[buf][u][8 * l + j];
+          const float cc = cr[j] * w.x - sr[j] * w.y, ss = sr[j] * w.x + cr[j] * w.y;
+          const float v = x[j], z = y[j];
+          x[j] = v * cc - z * ss;
+          y[j] = z * cc + v * ss;
+        }
+      }
+      char* dst = token_at(a, s, t < len && in_table(a.pool, t) ? checked(a.pool, entry[u]) : -1, t);
+      if (dst) {
+        store8((TP*)dst + 8 * l, x);
+        store8((TP*)dst + a.hd / 2 + 8 * l, y);
+      }
+    }
+    buf ^= 1;
+  }
+}
+
+// More stages than LDS holds: a chunk of 64 S tokens keeps its sums in
+// registers and goes through the stages; a stage's codewords are written to
+// one LDS buffer while the tokens gather from the other.  Sixteen lanes share
+// a token, four dimensions each (lanes 0-7 the lower half), so that every
+// gather, whatever the codes, touches every bank once.  SHARED (d >= 32, K <= 256): the
+// eight lanes of a half share a code; each of them holds that of one stage,
+// and two DPP broadcasts hand it out when its turn comes.
+constexpr int PS_THREADS = 1024;
+constexpr int PS_ROWS = PS_THREADS / 16;
+constexpr int PS_K = 256;
+constexpr int PS_BUF = PS_K * 16;           // f4 per buffer
+
+template <typename TP, int S, bool SHARED>
+__global__ void __launch_bounds__(PS_THREADS) paged_row_decode_stages_kernel(RestoreArgs a,
+                                                                             int nsub) {
+  extern __shared__ __align__(16) f4 tab[];                 // [2][PS_BUF]
+  __shared__ float2 turns[S][32];
+  const int tid = threadIdx.x, l = tid & 15, rg = tid >> 4;
+  const Slice s = slice_of<TP>(a, blockIdx.x % nsub);
+  const int per = (a.cap + PS_ROWS * S - 1) / (PS_ROWS * S);
+  const int chunk = blockIdx.x / nsub;
+  const int b = chunk / per, t0 = (chunk - b * per) * PS_ROWS * S;
+  const int len = min(a.seq_len[b], a.cap);
+  if (t0 >= len) return;
+  const int nrows = len - t0;
+  const int e = (l < 8 ? s.lo : s.hi - 32) + 4 * l, g = e / a.d;
+  if (s.turn) {
+    for (int i = tid; i < 32 * S; i += PS_THREADS) {
+      float2 x;
+      turn_of(t0 + PS_ROWS * (i >> 5), a.theta[s.first + (i & 31)], x.x, x.y);
+      turns[i >> 5][i & 31] = x;
+    }
+  }
+  constexpr int PER = PS_BUF / PS_THREADS;
+  f4 v[PER];
+  float gk[PER];
+  auto load = [&](int m) {
+    const float* gb = s.gain + ((int64_t)m * a.G + g) * a.K;
+    const float* sb = s.shape + ((int64_t)m * a.G + g) * a.K * a.d + (e - g * a.d);
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const uint32_t k = (uint32_t)min(u * PS_ROWS + rg, a.K - 1);
+      gk[u] = gb[k];
+      v[u] = *(const f4*)(sb + k * (uint32_t)a.d);
+    }
+  };
+  auto store = [&](f4* to) {
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int u = 0; u < PER; ++u) to[u * PS_THREADS + tid] = gk[u] * v[u];
+  };
+  f4 acc[S];
+#pragma unroll
+  for (int u = 0; u < S; ++u) acc[u] = (f4){0.f, 0.f, 0.f, 0.f};
+  int code[S];
+  const uint32_t* rows = s.codes + ((int64_t)b * a.cap + t0) * a.words;
+  load(0);
+  for (int m = 0; m < a.M; ++m) {
+    f4* from = tab + (m & 1) * PS_BUF;
+    if (!SHARED || (m & 7) == 0) {
+      // (the row opaque: addresses are formed here, not kept across stages)
+      int r = rg;
+      asm volatile("" : "+v"(r));
+      const int mm = SHARED ? min(m + (l & 7), a.M - 1) : m;
+      const int64_t bit = ((int64_t)mm * a.G + g) * a.b;
+#pragma unroll
+      for (int u = 0; u < S; ++u)
+        code[u] = code_at(rows + (int64_t)min(u * PS_ROWS + r, nrows - 1) * a.words, bit, a.b);
+    }
+    store(from);
+    if (m + 1 < a.M) load(m + 1);
+    // one barrier a stage: who writes stage m + 2 over this buffer has passed
+    // stage m + 1's, which all reach only after their gathers of stage m
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < S; ++u) {
+      int k = code[u];
+      if (SHARED) {
+        k = __builtin_amdgcn_update_dpp(k, code[u], 0x150, 0xf, 0x3, false);   // lane 0 to 0-7
+        k = __builtin_amdgcn_update_dpp(k, code[u], 0x158, 0xf, 0xc, false);   // lane 8 to 8-15
+        code[u] = __builtin_amdgcn_update_dpp(0, code[u], 0x12f, 0xf, 0xf, true);
+      }
+      acc[u] += from[k * 16 + l];
+    }
+  }
+  float cr[4], sr[4];
+  if (s.turn) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) turn_of(rg, a.theta[s.first + 4 * (l & 7) + j], cr[j], sr[j]);
+  }
+#pragma unroll
+  for (int u = 0; u < S; ++u) {
+    const int t = t0 + u * PS_ROWS + rg;
+    float x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = acc[u][j];
+    if (s.turn) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        // the element that this one is turned with: eight lanes on
+        const float z = __uint_as_float(
+            __builtin_amdgcn_update_dpp(0u, __float_as_uint(acc[u][j]), 0x128, 0xf, 0xf, true));
+        const float2 w = turns[u][4 * (l & 7) + j];
+        const float cc = cr[j] * w.x - sr[j] * w.y, ss = sr[j] * w.x + cr[j] * w.y;
+        x[j] = x[j] * cc + (l < 8 ? -z : z) * ss;
+      }
+    }
+    if (t >= len) continue;
+    char* dst = token_at(a, s, page_of(a.pool, b, t), t);
+    if (!dst) continue;
+    typedef TP v4 __attribute__((ext_vector_type(4)));
+    v4 r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = (TP)x[j];
+    *(v4*)((TP*)dst + (l < 8 ? 0 : a.hd / 2 - 32) + 4 * l) = r;
+  }
+}
+
+// Codebooks of more than 512 codewords, which LDS does not hold: a lane per 16
+// elements of a head of one token's key or value row, codewords from memory.
 template <typename TP>
 __global__ void __launch_bounds__(PA_THREADS) paged_row_decode_kernel(RestoreArgs a) {
   const int L = a.hd / 16;
@@ -217,6 +485,55 @@ gsrq_status append_launch(const AppendArgs& a, int hd, hipStream_t st) {
   if (hd == 64) paged_append_kernel<TI, TP, 64><<<grid, PA_THREADS, 0, st>>>(a);
   else if (hd == 128) paged_append_kernel<TI, TP, 128><<<grid, PA_THREADS, 0, st>>>(a);
   else paged_append_kernel<TI, TP, 256><<<grid, PA_THREADS, 0, st>>>(a);
+  return launch_ok();
+}
+
+template <typename TP> gsrq_status restore_launch(const RestoreArgs& a, hipStream_t st) {
+  const int64_t B = a.pool.B, nsub = 2ll * a.pool.Hkv * (a.hd / 64);
+  const int64_t table = (int64_t)a.M * a.K * 256;
+  if (table <= PR_TABLE) {
+    // two workgroups per CU where two tables fit, each with its share of the chunks
+    const int64_t chunks = B * ((a.cap + PR_CHUNK - 1) / PR_CHUNK);
+    const int64_t wgs = table <= PR_TABLE / 2 ? 512 : 256;
+    const int64_t ranges = std::max<int64_t>(1, std::min(wgs / nsub, chunks));
+    if (nsub * ranges > MAX_BLOCKS) return GSRQ_E_UNSUPPORTED;
+    auto kern = paged_decode_lds_kernel<TP>;
+    if (table > 65536 - 4096 &&
+        hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize,
+                            (int)table) != hipSuccess)
+      return GSRQ_E_HIP;
+    kern<<<(unsigned)(nsub * ranges), PR_THREADS, (size_t)table, st>>>(a, (int)nsub, (int)ranges);
+    return launch_ok();
+  }
+  if (a.K <= PS_K) {
+    // chunks of 768 tokens (fewer fills of the stages' buffers) where they
+    // give every CU a workgroup, else of 128
+    constexpr int LONG = 12, SHORT = 2;
+    const int64_t longs = nsub * B * ((a.cap + PS_ROWS * LONG - 1) / (PS_ROWS * LONG));
+    const int64_t shorts = nsub * B * ((a.cap + PS_ROWS * SHORT - 1) / (PS_ROWS * SHORT));
+    const bool is_long = longs >= 256;
+    const int64_t blocks = is_long ? longs : shorts;
+    if (blocks > (1 << 22) - 1) return GSRQ_E_UNSUPPORTED;   // of 1024 threads
+    const int lds = 2 * PS_BUF * (int)sizeof(f4);
+    auto go = [&](auto kern) -> gsrq_status {
+      if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds) !=
+          hipSuccess)
+        return GSRQ_E_HIP;
+      kern<<<(unsigned)blocks, PS_THREADS, lds, st>>>(a, (int)nsub);
+      return launch_ok();
+    };
+    const bool shared = a.d >= 32;
+    if (is_long)
+      return shared ? go(paged_row_decode_stages_kernel<TP, LONG, true>)
+                    : go(paged_row_decode_stages_kernel<TP, LONG, false>);
+    return shared ? go(paged_row_decode_stages_kernel<TP, SHORT, true>)
+                  : go(paged_row_decode_stages_kernel<TP, SHORT, false>);
+  }
+  const int64_t items = (int64_t)a.cap * a.pool.Hkv * (a.hd / 16);
+  const int64_t blocks = (items + PA_THREADS - 1) / PA_THREADS;
+  if (blocks > MAX_BLOCKS || B > 65535) return GSRQ_E_UNSUPPORTED;
+  paged_row_decode_kernel<TP>
+      <<<dim3((unsigned)blocks, 2, (unsigned)B), PA_THREADS, 0, st>>>(a);
   return launch_ok();
 }
 
@@ -306,17 +623,9 @@ gsrq_status gsrq_paged_restore(const gsrq_pages* pages, const gsrq_shape* kv, in
   a.K = kv->K;
   a.b = log2i(kv->K);
   a.hd = pages->head_dim;
-  const int64_t items = (int64_t)cap * pages->Hkv * (a.hd / 16);
-  const int64_t blocks = (items + PA_THREADS - 1) / PA_THREADS;
-  if (blocks > MAX_BLOCKS || pages->B > 65535) return GSRQ_E_UNSUPPORTED;
   hipStream_t st = (hipStream_t)stream;
   TimedLaunch tl(GSRQ_KERNEL_DECODE, st);
-  const dim3 grid((unsigned)blocks, 2, (unsigned)pages->B);
-  if (pages->dtype == GSRQ_F16)
-    paged_row_decode_kernel<_Float16><<<grid, PA_THREADS, 0, st>>>(a);
-  else
-    paged_row_decode_kernel<__bf16><<<grid, PA_THREADS, 0, st>>>(a);
-  return launch_ok();
+  return pages->dtype == GSRQ_F16 ? restore_launch<_Float16>(a, st) : restore_launch<__bf16>(a, st);
 }
 
 }  // extern "C"

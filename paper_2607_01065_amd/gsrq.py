@@ -11,6 +11,7 @@ import contextlib
 import ctypes
 import math
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional
 
@@ -118,14 +119,13 @@ def load_library(path: str = LIB_PATH):
     lib.gsrq_attn_decode_noalloc.restype = ctypes.c_int
     lib.gsrq_attn_decode_noalloc.argtypes = [AP, SP, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                              ctypes.c_int, _vp, _vp]
-    PP, HP = ctypes.POINTER(Pages), ctypes.POINTER(Heads)
+    PP = HP = XP = _vp               # packed structures, or byref() of Pages, Heads, PagedAttn
     lib.gsrq_paged_append.restype = ctypes.c_int
     lib.gsrq_paged_append.argtypes = [PP, ctypes.c_int64, _vp, _vp, HP, HP, HP, ctypes.c_int32,
                                       ctypes.c_int, _vp, _vp, _vp, ctypes.c_float, _vp, _vp]
     lib.gsrq_paged_restore.restype = ctypes.c_int
     lib.gsrq_paged_restore.argtypes = [PP, SP, ctypes.c_int32, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                        _vp, _vp]
-    XP = ctypes.POINTER(PagedAttn)
     lib.gsrq_attn_paged_workspace_bytes.restype = ctypes.c_int
     lib.gsrq_attn_paged_workspace_bytes.argtypes = [XP, PP, ctypes.POINTER(ctypes.c_size_t)]
     lib.gsrq_attn_paged.restype = ctypes.c_int
@@ -265,7 +265,7 @@ def _need(t, name, dtypes, device, shape=None):
         raise ValueError(f"{name} is on {t.device}, expected {device}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if shape is not None and t.numel() != int(np.prod(shape)):
+    if shape is not None and t.numel() != math.prod(shape):
         raise ValueError(f"{name} has {t.numel()} elements, expected {tuple(shape)}")
 
 
@@ -557,65 +557,81 @@ def attn_decode(k_codes, v_codes, seq_len, k_gain, k_shape, v_gain, v_shape, q, 
 
 # ------------------------------------------------------------- paged cache
 
-def _paged_dtype(t, name) -> int:
+# The structures of the calls of every decoding step are packed, not built
+# field by field (a few microseconds of a call); layouts as Pages, Heads and
+# PagedAttn above.
+_PAGES = struct.Struct("@PP3q3qPq7i0q")
+_HEADS = struct.Struct("@Pqq")
+_PAGED_ATTN = struct.Struct("@qiifI0q")
+_NO_CONTEXT = contextlib.nullcontext()
+
+
+def _paged_types():
     torch = _torch()
-    if t.dtype == torch.bfloat16:
-        return GSRQ_BF16
-    try:
-        return _dtype_code(t)
-    except TypeError:
-        raise TypeError(f"{name} must be float16, bfloat16 or float32, not {t.dtype}") from None
+    return {torch.float16: GSRQ_F16, torch.bfloat16: GSRQ_BF16, torch.float32: GSRQ_F32}
 
 
-def _on(device, stream):
-    """Context of a paged call: its stream's device is current and its new
-    tensors come from its stream's memory, so that a workspace freed when the
+def _paged_dtype(t, name) -> int:
+    code = _paged_types().get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float16, bfloat16 or float32, not {t.dtype}")
+    return code
+
+
+def _paged_device(device, stream):
+    """Context of a paged call, or None where the device is current and the
+    stream its current one: the stream's device is made current and new
+    tensors come from the stream's memory, so that a workspace freed when the
     call returns is not handed to another stream while it is in use."""
     torch = _torch()
     if device.type != "cuda":
         raise ValueError(f"the tensors are on {device}, expected a GPU")
     if stream is None:
-        if device.index == torch.cuda.current_device():
-            return contextlib.nullcontext()
-        return torch.cuda.device(device)
+        current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        return None if device.index == current() else torch.cuda.device(device)
     if stream.device != device:
         raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
     return torch.cuda.stream(stream)
 
 
-def _pages(k_pages, v_pages, table) -> Pages:
+def _pages(k_pages, v_pages, table) -> bytes:
+    """gsrq_pages of two pools [pages, page_size, Hkv, head_dim] and their table."""
     torch = _torch()
-    if k_pages.dim() != 4 or v_pages.shape != k_pages.shape:
+    shape, dtype, dev = k_pages.shape, k_pages.dtype, k_pages.device
+    if len(shape) != 4 or v_pages.shape != shape:
         raise ValueError("k_pages and v_pages must be [pages, page_size, Hkv, head_dim], both alike")
-    dev = k_pages.device
-    if k_pages.dtype not in (torch.float16, torch.bfloat16) or v_pages.dtype != k_pages.dtype:
+    if dtype is not torch.float16 and dtype is not torch.bfloat16 or v_pages.dtype is not dtype:
         raise TypeError("pages must be float16 or bfloat16, both alike")
-    if table.dim() != 2 or table.dtype != torch.int32:
+    if table.dim() != 2 or table.dtype is not torch.int32:
         raise TypeError("table must be a 2-D int32 tensor")
     if v_pages.device != dev or table.device != dev:
         raise ValueError(f"v_pages and table must be on {dev}")
-    ks, vs, ts = k_pages.stride(), v_pages.stride(), table.stride()
-    if ks[3] != 1 or vs[3] != 1 or (ts[1] != 1 and table.shape[1] > 1):
-        raise ValueError("elements of a head and entries of a table row must be adjacent")
-    n, size, Hkv, hd = k_pages.shape
+    k0, k1, k2, k3 = k_pages.stride()
+    v0, v1, v2, v3 = v_pages.stride()
+    t0, t1 = table.stride()
     B, per = table.shape
-    S3 = ctypes.c_int64 * 3
-    return Pages(k_pages.data_ptr(), v_pages.data_ptr(), S3(*ks[:3]), S3(*vs[:3]), table.data_ptr(),
-                 max(ts[0], per), n, size, per, B, Hkv, hd,
-                 GSRQ_BF16 if k_pages.dtype == torch.bfloat16 else GSRQ_F16)
+    if k3 != 1 or v3 != 1 or (t1 != 1 and per > 1):
+        raise ValueError("elements of a head and entries of a table row must be adjacent")
+    n, size, Hkv, hd = shape
+    if max(n, size, Hkv, hd, B, per) >= 1 << 31:
+        raise ValueError("a dimension of the pages or the table does not fit 32 bits")
+    return _PAGES.pack(k_pages.data_ptr(), v_pages.data_ptr(), k0, k1, k2, v0, v1, v2,
+                       table.data_ptr(), t0 if B > 1 else per, n, size, per, B, Hkv, hd,
+                       GSRQ_F16 if dtype is torch.float16 else GSRQ_BF16)
 
 
-def _heads(x, name, heads, head_dim, rows, dtype, device) -> Heads:
-    if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim or x.shape[0] != rows:
+def _heads(x, name, heads, head_dim, rows, dtype, device) -> bytes:
+    """gsrq_heads of rows [rows, heads, head_dim]."""
+    if x.shape != (rows, heads, head_dim):
         raise ValueError(f"{name} must be [{rows}, {heads}, {head_dim}], not {tuple(x.shape)}")
-    if x.dtype != dtype:
+    if x.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {x.dtype}")
     if x.device != device:
         raise ValueError(f"{name} is on {x.device}, expected {device}")
-    s = x.stride()
-    if s[2] != 1:
+    s0, s1, s2 = x.stride()
+    if s2 != 1:
         raise ValueError(f"{name}: elements of a head must be adjacent")
-    return Heads(x.data_ptr(), s[0], s[1])
+    return _HEADS.pack(x.data_ptr(), s0, s1)
 
 
 def paged_append(k, v, k_pages, v_pages, table, q_start, seq_len, *, q=None, theta=None,
@@ -631,17 +647,18 @@ def paged_append(k, v, k_pages, v_pages, table, q_start, seq_len, *, q=None, the
     Returns the queries [T, Hq, head_dim] in the pages' type, or None
     without q."""
     torch = _torch()
-    lib = load_library()
+    lib = _lib or load_library()
     pages = _pages(k_pages, v_pages, table)
-    dev, hd, B = k_pages.device, pages.head_dim, pages.B
-    T = k.shape[0]
+    dev, B = k_pages.device, table.shape[0]
+    Hkv, hd = k_pages.shape[2:]
+    T, dtype = k.shape[0], k.dtype
     dt = _paged_dtype(k, "k")
-    kh = _heads(k, "k", pages.Hkv, hd, T, k.dtype, dev)
-    vh = _heads(v, "v", pages.Hkv, hd, T, k.dtype, dev)
-    Hq = 0
+    kh = _heads(k, "k", Hkv, hd, T, dtype, dev)
+    vh = _heads(v, "v", Hkv, hd, T, dtype, dev)
+    Hq, qh = 0, None
     if q is not None:
         Hq = q.shape[1] if q.dim() == 3 else 0
-        qh = _heads(q, "q", Hq, hd, T, k.dtype, dev)
+        qh = _heads(q, "q", Hq, hd, T, dtype, dev)
     elif q_norm is not None or q_out is not None:
         raise ValueError("q_norm and q_out need q")
     _need(q_start, "q_start", (torch.int32,), dev, (B + 1,))
@@ -650,15 +667,14 @@ def paged_append(k, v, k_pages, v_pages, table, q_start, seq_len, *, q=None, the
     _need(k_norm, "k_norm", (torch.float32,), dev, (hd,))
     _need(q_norm, "q_norm", (torch.float32,), dev, (hd,))
     _need(q_out, "q_out", (k_pages.dtype,), dev, (T, Hq, hd))
-    with _on(dev, stream):
+    with _paged_device(dev, stream) or _NO_CONTEXT:
         if q is not None and q_out is None:
             q_out = torch.empty((T, Hq, hd), dtype=k_pages.dtype, device=dev)
         if T == 0:
             return q_out
         st = lib.gsrq_paged_append(
-            ctypes.byref(pages), T, _ptr(q_start), _ptr(seq_len), ctypes.byref(kh), ctypes.byref(vh),
-            None if q is None else ctypes.byref(qh), Hq, dt, _ptr(theta), _ptr(k_norm),
-            _ptr(q_norm), float(eps), _ptr(q_out), _append_stream_handle(stream))
+            pages, T, q_start.data_ptr(), seq_len.data_ptr(), kh, vh, qh, Hq, dt, _ptr(theta),
+            _ptr(k_norm), _ptr(q_norm), eps, _ptr(q_out), _append_stream_handle(stream))
     if st != GSRQ_OK:
         _check(st, "gsrq_paged_append")
     return q_out
@@ -667,11 +683,9 @@ def paged_append(k, v, k_pages, v_pages, table, q_start, seq_len, *, q=None, the
 def attn_paged_workspace_bytes(T, Hq, k_pages, v_pages, table, *, window=0) -> int:
     """Workspace of attn_paged for T rows of Hq query heads over these pages."""
     n = ctypes.c_size_t()
-    s = PagedAttn(int(T), int(Hq), int(window), 1.0, 0)
-    pages = _pages(k_pages, v_pages, table)
-    _check(load_library().gsrq_attn_paged_workspace_bytes(ctypes.byref(s), ctypes.byref(pages),
-                                                          ctypes.byref(n)),
-           "gsrq_attn_paged_workspace_bytes")
+    _check(load_library().gsrq_attn_paged_workspace_bytes(
+        _PAGED_ATTN.pack(int(T), int(Hq), int(window), 1.0, 0), _pages(k_pages, v_pages, table),
+        ctypes.byref(n)), "gsrq_attn_paged_workspace_bytes")
     return int(n.value)
 
 
@@ -684,35 +698,40 @@ def attn_paged(q, k_pages, v_pages, table, q_start, seq_len, *, scale=None, wind
     workspace: a uint8 tensor of attn_paged_workspace_bytes, or None (one is
     made for the call)."""
     torch = _torch()
-    lib = load_library()
+    lib = _lib or load_library()
     pages = _pages(k_pages, v_pages, table)
-    dev, hd, B = k_pages.device, pages.head_dim, pages.B
+    dev, B, hd = k_pages.device, table.shape[0], k_pages.shape[3]
     if q.dim() != 3:
         raise ValueError("q must be [T, Hq, head_dim]")
-    T, Hq = q.shape[0], q.shape[1]
-    qh = _heads(q, "q", Hq, hd, T, k_pages.dtype, dev)
+    T, Hq = q.shape[:2]
+    dtype = k_pages.dtype
+    qh = _heads(q, "q", Hq, hd, T, dtype, dev)
     _need(q_start, "q_start", (torch.int32,), dev, (B + 1,))
     _need(seq_len, "seq_len", (torch.int32,), dev, (B,))
-    _need(out, "out", (q.dtype,), dev, (T, Hq, hd))
+    _need(out, "out", (dtype,), dev, (T, Hq, hd))
     if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
         raise ValueError(f"workspace must be contiguous, on {dev}")
-    scale = 1.0 / math.sqrt(hd) if scale is None else float(scale)
-    s = PagedAttn(T, Hq, int(window), scale, 0)
-    with _on(dev, stream):
+    if not 0 <= window < 1 << 31:
+        raise ValueError("window must be a number of tokens, or 0")
+    s = _PAGED_ATTN.pack(T, Hq, window, hd ** -0.5 if scale is None else scale, 0)
+    with _paged_device(dev, stream) or _NO_CONTEXT:
         if out is None:
-            out = torch.empty((T, Hq, hd), dtype=q.dtype, device=dev)
+            out = torch.empty((T, Hq, hd), dtype=dtype, device=dev)
         total = torch.empty((T, Hq), dtype=torch.float32, device=dev) if lse else None
         if T > 0:
             n = ctypes.c_size_t()
-            _check(lib.gsrq_attn_paged_workspace_bytes(ctypes.byref(s), ctypes.byref(pages),
-                                                       ctypes.byref(n)),
-                   "gsrq_attn_paged_workspace_bytes")
-            ws = _workspace(n.value, dev, workspace) if n.value else None
-            st = lib.gsrq_attn_paged(
-                ctypes.byref(s), ctypes.byref(pages), _ptr(q_start), _ptr(seq_len),
-                ctypes.byref(qh), _ptr(out), _ptr(total), _ptr(ws),
-                0 if ws is None else ws.numel() * ws.element_size(), _append_stream_handle(stream))
-            _check(st, "gsrq_attn_paged")
+            st = lib.gsrq_attn_paged_workspace_bytes(s, pages, ctypes.byref(n))
+            if st != GSRQ_OK:
+                _check(st, "gsrq_attn_paged_workspace_bytes")
+            ws, size = None, n.value
+            if size:
+                ws = _workspace(size, dev, workspace)
+                size = ws.numel() * ws.element_size()
+            st = lib.gsrq_attn_paged(s, pages, q_start.data_ptr(), seq_len.data_ptr(), qh,
+                                     out.data_ptr(), _ptr(total), _ptr(ws), size,
+                                     _append_stream_handle(stream))
+            if st != GSRQ_OK:
+                _check(st, "gsrq_attn_paged")
     return (out, total) if lse else out
 
 
@@ -725,13 +744,13 @@ def paged_restore(k_codes, v_codes, seq_len, k_gain, k_shape, v_gain, v_shape, k
     torch = _torch()
     lib = load_library()
     pages = _pages(k_pages, v_pages, table)
-    dev = k_pages.device
+    dev, hd = k_pages.device, k_pages.shape[3]
     if k_codes.dim() != 3 or k_shape.dim() != 4:
         raise ValueError("codes must be [B, cap, W] and codebook shapes [M, G, K, d]")
     B, cap, W = k_codes.shape
     M, G, K, d = k_shape.shape
-    if B != pages.B:
-        raise ValueError(f"codes of {B} sequences, a table of {pages.B}")
+    if B != table.shape[0]:
+        raise ValueError(f"codes of {B} sequences, a table of {table.shape[0]}")
     sh = make_shape(max(B * cap, 1), G * d, d, K, M)
     words = int(lib.gsrq_code_words(ctypes.byref(sh)))
     if W != words:
@@ -742,12 +761,12 @@ def paged_restore(k_codes, v_codes, seq_len, k_gain, k_shape, v_gain, v_shape, k
     for name, t, size in (("k_gain", k_gain, (M, G, K)), ("k_shape", k_shape, (M, G, K, d)),
                           ("v_gain", v_gain, (M, G, K)), ("v_shape", v_shape, (M, G, K, d))):
         _need(t, name, (torch.float32,), dev, size)
-    _need(theta, "theta", (torch.float64,), dev, (pages.head_dim // 2,))
+    _need(theta, "theta", (torch.float64,), dev, (hd // 2,))
     if cap == 0:
         return
-    with _on(dev, stream):
+    with _paged_device(dev, stream) or _NO_CONTEXT:
         st = lib.gsrq_paged_restore(
-            ctypes.byref(pages), ctypes.byref(sh), cap, _ptr(k_codes), _ptr(v_codes),
+            pages, ctypes.byref(sh), cap, _ptr(k_codes), _ptr(v_codes),
             _ptr(seq_len), _ptr(k_gain), _ptr(k_shape), _ptr(v_gain), _ptr(v_shape), _ptr(theta),
             _append_stream_handle(stream))
     _check(st, "gsrq_paged_restore")

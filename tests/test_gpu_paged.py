@@ -168,10 +168,16 @@ def _books(M, G, K, d, seed):
     ([20], 20, 4, 128, 256, 4096, 2, 32, "f16", True),              # a codeword over two heads, 12-bit codes
     ([70, 65], 70, 2, 256, 8, 256, 2, 16, "bf16", True),
     ([25], 30, 2, 256, 32, 2, 5, 8, "f16", True),
+    ([1500, 3, 900], 1500, 2, 64, 8, 256, 1, 16, "f16", True),      # several chunks, ranges over sequences
+    ([700], 700, 1, 128, 16, 256, 4, 16, "f16", True),              # more stages than LDS holds, codes of their own
+    ([800, 10], 801, 8, 128, 128, 256, 20, 32, "bf16", True),       # past 16 stages, chunks of 768
+    ([130], 130, 1, 256, 64, 16, 40, 8, "f16", True),               # 4-bit codes, 40 stages
+    ([60], 60, 2, 64, 32, 512, 1, 8, "bf16", True),                 # 9-bit codes
 ])
 def test_restore(lens, cap, Hkv, hd, d, K, M, page, held, rope):
-    """Codes of both sides into pages.  Tolerance: half a step of the type, the rotation as above (its 9 roundings
-    under 2^-19), and M roundings of a codeword and of the float32 sum: 2 M 2^-24 of the codewords' magnitudes."""
+    """Codes of both sides into pages.  Tolerance: half a step of the type; a rotation's, whose cosine and sine may come
+    from two rotations joined (6 roundings each and 3 of the product) and which adds 3: 18 under 2^-19; and M
+    roundings of a codeword and of the float32 sum: 2 M 2^-24 of the codewords' magnitudes."""
     say("restore", lens, cap, Hkv, hd, d, K, M, page, held)
     Bn, G = len(lens), Hkv * hd // d
     rng = np.random.default_rng(3)
