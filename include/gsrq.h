@@ -406,8 +406,8 @@ gsrq_status gsrq_attn_decode_noalloc(const gsrq_attn_shape* a, const gsrq_shape*
  * table (a shared prompt); a call that writes one token of a page from two
  * rows leaves either.
  * This build: head_dim 64, 128 or 256, page_size a power of two from 8 on,
- * float16 or bfloat16 pages, tokens less than 2^26 elements apart (other
- * valid shapes GSRQ_E_UNSUPPORTED); per * page_size at
+ * float16 or bfloat16 pages, tokens less than 2^26 and pages less than 2^31
+ * elements apart (other valid shapes GSRQ_E_UNSUPPORTED); per * page_size at
  * most 2^30; k and v 16-byte aligned, strides multiples of 8 elements.
  */
 typedef struct {

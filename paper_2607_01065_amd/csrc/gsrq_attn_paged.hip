@@ -104,7 +104,7 @@ __device__ __forceinline__ Seq sequence(const PtArgs& a, int b) {
 }
 
 __device__ __forceinline__ bool is_few(const PtArgs& a, const Seq& s) {
-  return (int64_t)s.n * a.GQ <= PT_FEW;
+  return s.n * a.GQ <= PT_FEW;                                  // (T GQ < 2^30)
 }
 
 // What queries r0 .. r0 + rows - 1 of a sequence read: keys lo .. hi - 1, in
@@ -115,10 +115,9 @@ struct Span {
 
 __device__ __forceinline__ Span span_of(const PtArgs& a, const Seq& s, int r0, int rows, int unit,
                                         int ns) {
-  const int64_t most = (int64_t)s.n * a.GQ - 1;
-  const int64_t last = r0 + rows - 1 < most ? r0 + rows - 1 : most;
-  const int64_t top = s.pos0 + last / a.GQ + 1;
-  const int64_t bottom = a.window ? s.pos0 + r0 / a.GQ - a.window + 1 : 0;
+  const uint32_t last = min(r0 + rows, s.n * a.GQ) - 1;        // (T GQ < 2^30)
+  const int64_t top = s.pos0 + last / (uint32_t)a.GQ + 1;
+  const int64_t bottom = a.window ? s.pos0 + (uint32_t)r0 / (uint32_t)a.GQ - a.window + 1 : 0;
   Span w;
   w.hi = (int)(top < s.keys ? top : s.keys);
   w.lo = bottom > 0 ? (int)(bottom < s.keys ? bottom : s.keys) / unit * unit : 0;
@@ -233,7 +232,7 @@ template <typename T, int HD> struct Columns {
   __device__ __forceinline__ void start(const PtArgs& a, const Seq& s, int head, int r) {
     const int half = (threadIdx.x >> 5) & 1;
     const bool real = r < s.n * a.GQ;
-    const int tok = real ? r / a.GQ : 0, g = real ? r - tok * a.GQ : 0;
+    const int tok = real ? (uint32_t)r / (uint32_t)a.GQ : 0, g = real ? r - tok * a.GQ : 0;
     const int64_t pos = s.pos0 + tok;
     see_hi = real ? (int)(pos + 1 < s.keys ? (pos + 1 > 0 ? pos + 1 : 0) : s.keys) : 0;
     const int64_t from = a.window ? pos - a.window + 1 : 0;
@@ -263,13 +262,10 @@ template <typename T, int HD> struct Columns {
     l = 0.f;
   }
 
-  // The weights of NB blocks of 32 keys from key t0 on, the keys in LDS.
-  // absent: rows of the tile that nobody sees.
+  // Scores of NB blocks of 32 keys in LDS.
   template <int NB>
-  __device__ __forceinline__ void weights(const PtArgs& a, const char* kt, int t0, uint64_t absent,
-                                          v8 (&p)[NB][2]) {
+  __device__ __forceinline__ void scores(const char* kt, f16v (&sc)[NB]) {
     const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
-    f16v sc[NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -281,17 +277,17 @@ template <typename T, int HD> struct Columns {
         const v8 kf = *(const v8*)(kt + key_at<HD>(32 * n + col, 2 * k + half));
         sc[n] = Vec<T>::mfma(kf, q[k], sc[n]);
       }
-    // keys are read four products ahead
-    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-    for (int i = 0; i < KS * NB - 4; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    }
-    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+  }
+
+  // Masks the scores of the keys from t0 on (absent: rows that nobody sees)
+  // and raises the maximum in use where they exceed it.
+  template <int NB>
+  __device__ __forceinline__ void settle(const PtArgs& a, int t0, uint64_t absent,
+                                         f16v (&sc)[NB]) {
     if (absent || t0 + 32 * NB > all_hi || t0 < all_lo) {
       // (bounds moved to the lane's first row, so that each element compares
       // with a constant)
+      const int half = (threadIdx.x >> 5) & 1;
       const int hi = see_hi - t0 - 4 * half, lo = see_lo - t0 - 4 * half;
       const uint64_t gone = absent >> (4 * half);
 #pragma unroll
@@ -318,6 +314,12 @@ template <typename T, int HD> struct Columns {
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] *= f;
     }
+  }
+
+  // Weights of settled scores.
+  template <int NB>
+  __device__ __forceinline__ void weights(const PtArgs& a, const f16v (&sc)[NB],
+                                          v8 (&p)[NB][2]) {
     const float sub = m == -INFINITY ? 0.f : PT_SHIFT - m;
 #pragma unroll
     for (int n = 0; n < NB; ++n)
@@ -342,14 +344,6 @@ template <typename T, int HD> struct Columns {
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[t] = Vec<T>::mfma(values(vt, n, k, t), p[n][k], o[t]);
-    // values are read two products ahead
-    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-    for (int i = 0; i < 2 * NB * DT - 2; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-    }
-    __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
   }
 
   // V^T of 32 dimensions and the 16 tokens of weights [n][k], in their order.
@@ -412,14 +406,22 @@ template <typename T> __device__ __forceinline__ bool without_infinities(u4* at)
   return any;
 }
 
-// First token of a group of rows in one page (pages hold at least 8 tokens, a
-// wave's load takes 64 / CH <= 8 rows): address of one head's keys or values.
-// For an absent page the pool's first tokens, which nobody looks at.
-template <typename T>
-__device__ __forceinline__ const char* rows_of(const PagePool& p, const char* base,
-                                               const int64_t (&st)[3], int page, int t, int head) {
-  const int64_t in = page < 0 ? 0 : t & ((1 << p.shift) - 1);
-  return base + sizeof(T) * ((page < 0 ? 0 : page) * st[0] + in * st[1] + head * st[2]);
+// Where a lane's token lies from its head's first key (or value) on, in bytes;
+// an absent page counts as the pool's first, which nobody looks at.  Taken one
+// token a lane, so that a load of several rows needs two lane reads and an
+// addition, not their products: pages hold at least 8 tokens, and a wave's
+// load of 64 / CH <= 8 rows lies in one.
+__device__ __forceinline__ uint64_t token_offset(const PagePool& p, const int64_t (&st)[3], int page,
+                                                 int t) {
+  const uint32_t in = page < 0 ? 0 : t & ((1 << p.shift) - 1);
+  return 2 * ((uint64_t)(uint32_t)(page < 0 ? 0 : page) * (uint32_t)st[0] +
+              (uint64_t)in * (uint32_t)st[1]);
+}
+// base + the offset that lane `row` holds.
+__device__ __forceinline__ const char* rows_at(const char* base, uint64_t offset, int row) {
+  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)offset, row);
+  const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(offset >> 32), row);
+  return base + ((uint64_t)hi << 32 | lo);
 }
 
 // A row's result, from its lane's part of the sums (both halves of l joined).
@@ -483,36 +485,50 @@ __device__ __forceinline__ void many(const PtArgs& a, char* lds, int block) {
     odd_tiles[1] = -1;
   }
 
-  // tile t0 to LDS, pages found one a lane; a wave's load fills 1 KiB
-  constexpr int RL = 64 / C::CH;                       // rows of one load
+  // a tile's keys or values to LDS, pages found one a lane; a wave's load fills
+  // 1 KiB
+  constexpr int NB = C::TN / 32, RL = 64 / C::CH;      // RL: rows of one load
   const int lrow = lane / C::CH, lch = lane % C::CH;
-  auto fetch = [&](int t0, int page, const char* kt) {
+  const char* const kbase = a.pool.k + sizeof(T) * head * a.pool.ks[2];
+  const char* const vbase = a.pool.v + sizeof(T) * head * a.pool.vs[2];
+  auto fetch = [&](bool key, int t0, int page, const char* at) __attribute__((always_inline)) {
+    const int64_t (&st)[3] = key ? a.pool.ks : a.pool.vs;
+    const uint64_t offset = token_offset(a.pool, st, page, t0 + (lane & (C::TN - 1)));
 #pragma unroll
     for (int u = 0; u < C::PER; ++u) {
       const int row = (u * PT_WAVES + wave) * RL;
-      const int pg = __builtin_amdgcn_readlane(page, row);
-      const uint32_t to = lds_offset(kt) + 1024 * (u * PT_WAVES + wave);
-      load_to_lds(rows_of<T>(a.pool, a.pool.k, a.pool.ks, pg, t0 + row, head),
-                  2 * (lrow * (uint32_t)a.pool.ks[1] + 8 * key_chunk<HD>(row + lrow, lch)), to);
-      load_to_lds(rows_of<T>(a.pool, a.pool.v, a.pool.vs, pg, t0 + row, head),
-                  2 * (lrow * (uint32_t)a.pool.vs[1] + 8 * value_chunk<HD>(row + lrow, lch)),
-                  to + C::BYTES);
+      const int ch = key ? key_chunk<HD>(row + lrow, lch) : value_chunk<HD>(row + lrow, lch);
+      load_to_lds(rows_at(key ? kbase : vbase, offset, row),
+                  2 * (lrow * (uint32_t)st[1] + 8 * ch),
+                  lds_offset(at) + 1024 * (u * PT_WAVES + wave));
     }
   };
   const int mine = lane & (C::TN - 1);
-  int entry = entry_of(a.pool, b, begin + mine);
-  int page = begin + mine < end ? checked(a.pool, entry) : -1;
-  uint64_t absent = __ballot(page < 0), next_absent = 0;
-  __syncthreads();                                     // odd_tiles
-  fetch(begin, page, lds);
-  entry = entry_of(a.pool, b, begin + C::TN + mine);
-  int odd = 0;
-  for (int t0 = begin; t0 < end; t0 += C::TN, odd ^= 1, absent = next_absent) {
-    char* kt = lds + odd * 2 * C::BYTES;
-    char* vt = kt + C::BYTES;
-    const bool masked = absent || t0 + C::TN > wg_hi || t0 < wg_lo;
-    wait_loads<0>();
-    if (masked) {
+  auto page_at = [&](int t0, int entry) __attribute__((always_inline)) {
+    return t0 + mine < end ? checked(a.pool, entry) : -1;
+  };
+  // Keys run one tile ahead of values: while a tile's weights are taken and its
+  // values added, the next one's scores are formed, so that the matrix unit
+  // works through the exponentials.
+  char* const kt = lds;
+  char* const vt = lds + 2 * C::BYTES;
+  int page = page_at(begin, entry_of(a.pool, b, begin + mine));
+  int next = page_at(begin + C::TN, entry_of(a.pool, b, begin + C::TN + mine));
+  uint64_t absent = __ballot(page < 0), next_absent = __ballot(next < 0);
+  fetch(true, begin, page, kt);
+  wait_loads<0>();
+  __syncthreads();                                     // (odd_tiles, too)
+  fetch(false, begin, page, vt);
+  fetch(true, begin + C::TN, next, kt + C::BYTES);
+  int entry = entry_of(a.pool, b, begin + 2 * C::TN + mine);
+  f16v even_scores[NB], odd_scores[NB];
+  c.template scores<NB>(kt, even_scores);
+  c.template settle<NB>(a, begin, absent, even_scores);
+  auto step = [&](int t0, int odd, f16v (&sc)[NB], f16v (&ahead)[NB])
+                  __attribute__((always_inline)) {
+    char* const v = vt + odd * C::BYTES;
+    wait_loads<0>();                                   // values of t0, keys of the next
+    if (absent || t0 + C::TN > wg_hi || t0 < wg_lo) {
       // each thread looks at the values that it has loaded; rows of absent
       // pages become zeros
       // (opaque: addresses are formed here, not kept in registers)
@@ -521,27 +537,55 @@ __device__ __forceinline__ void many(const PtArgs& a, char* lds, int block) {
 #pragma unroll
       for (int u = 0; u < C::PER; ++u) {
         const int i = u * PT_THREADS + me, row = i / C::CH;
-        u4* v = (u4*)(vt + 16 * i);
+        u4* at = (u4*)(v + 16 * i);
         if ((absent >> row) & 1) {
-          *v = (u4){0u, 0u, 0u, 0u};
-        } else if (without_infinities<T>(v)) {
+          *at = (u4){0u, 0u, 0u, 0u};
+        } else if (without_infinities<T>(at)) {
           atomicMin(&odd_tiles[0], t0);
           atomicMax(&odd_tiles[1], t0);
         }
       }
     }
     wait_lds();
-    __builtin_amdgcn_s_barrier();                      // tile t0 is there, the other one free
+    __builtin_amdgcn_s_barrier();                      // both are there, the other halves free
     asm volatile("" : : : "memory");
+    page = next;
+    next = page_at(t0 + 2 * C::TN, entry);
+    absent = next_absent;
+    next_absent = __ballot(next < 0);
     if (t0 + C::TN < end) {
-      page = t0 + C::TN + mine < end ? checked(a.pool, entry) : -1;
-      next_absent = __ballot(page < 0);
-      fetch(t0 + C::TN, page, lds + (odd ^ 1) * 2 * C::BYTES);
-      entry = entry_of(a.pool, b, t0 + 2 * C::TN + mine);
+      fetch(false, t0 + C::TN, page, vt + (odd ^ 1) * C::BYTES);
+      fetch(true, t0 + 2 * C::TN, next, kt + odd * C::BYTES);
+      entry = entry_of(a.pool, b, t0 + 3 * C::TN + mine);
     }
-    typename Vec<T>::v8 p[C::TN / 32][2];
-    c.template weights<C::TN / 32>(a, kt, t0, absent, p);
-    c.template add_values<C::TN / 32>(vt, p);
+    // (past the last tile the scores are those of stale keys, never used)
+    typename Vec<T>::v8 p[NB][2];
+    c.template scores<NB>(kt + (odd ^ 1) * C::BYTES, ahead);
+    c.template weights<NB>(a, sc, p);
+    c.template add_values<NB>(v, p);
+    // one product of the scores, one key read, and a share of the weights in
+    // turn; then the values, read two products ahead
+    constexpr int N = NB * (HD / 16), W = NB * 16;     // products, weights
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if (i < N - 2) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 5 * W / (2 * N), 0);
+      __builtin_amdgcn_sched_group_barrier(0x400, W / N, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if (i < N - 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
+    if (t0 + C::TN < end) c.template settle<NB>(a, t0 + C::TN, absent, ahead);
+  };
+  for (int t0 = begin; t0 < end; t0 += 2 * C::TN) {
+    step(t0, 0, even_scores, odd_scores);
+    if (t0 + C::TN >= end) break;
+    step(t0 + C::TN, 1, odd_scores, even_scores);
   }
   __syncthreads();
   c.see_infinities(a, b, head, __builtin_amdgcn_readfirstlane(odd_tiles[0]),
@@ -596,14 +640,17 @@ __device__ __forceinline__ void few(const PtArgs& a, char* lds, int block) {
   // the keys or the values of tile t0 to LDS; pages found one a lane
   constexpr int RL = 64 / C::CH;                       // rows of one load
   const int lrow = lane / C::CH, lch = lane % C::CH;
-  auto fetch = [&](const char* base, const int64_t (&st)[3], int t0, int page, const char* at,
-                   bool key) {
+  const char* const kbase = a.pool.k + sizeof(T) * head * a.pool.ks[2];
+  const char* const vbase = a.pool.v + sizeof(T) * head * a.pool.vs[2];
+  auto fetch = [&](bool key, int t0, int page, const char* at) __attribute__((always_inline)) {
+    const int64_t (&st)[3] = key ? a.pool.ks : a.pool.vs;
+    const uint64_t offset = token_offset(a.pool, st, page, t0 + (lane & 31));
     const uint32_t to = lds_offset(at);
 #pragma unroll
     for (int u = 0; u < C::FEW_PER; ++u) {
-      const int row = u * RL, pg = __builtin_amdgcn_readlane(page, row);
+      const int row = u * RL;
       const int ch = key ? key_chunk<HD>(row + lrow, lch) : value_chunk<HD>(row + lrow, lch);
-      load_to_lds(rows_of<T>(a.pool, base, st, pg, t0 + row, head),
+      load_to_lds(rows_at(key ? kbase : vbase, offset, row),
                   2 * (lrow * (uint32_t)st[1] + 8 * ch), to + 1024 * u);
     }
   };
@@ -615,17 +662,20 @@ __device__ __forceinline__ void few(const PtArgs& a, char* lds, int block) {
   int page = page_at(begin, entry_of(a.pool, b, begin + mine));
   int next = page_at(begin + PT_FEW_UNIT, entry_of(a.pool, b, begin + PT_FEW_UNIT + mine));
   if (begin < end) {
-    fetch(a.pool.k, a.pool.ks, begin, page, kt, true);
-    fetch(a.pool.v, a.pool.vs, begin, page, vt, false);
+    fetch(true, begin, page, kt);
+    fetch(false, begin, page, vt);
   }
   for (int t0 = begin; t0 < end; t0 += PT_FEW_UNIT) {
     const uint64_t absent = __ballot(page < 0) & 0xffffffffull;
     wait_loads<C::FEW_PER>();                          // the keys are there
     const int after = entry_of(a.pool, b, t0 + 2 * PT_FEW_UNIT + mine);
+    f16v sc[1];
     typename Vec<T>::v8 p[1][2];
-    c.template weights<1>(a, kt, t0, absent, p);
+    c.template scores<1>(kt, sc);
+    c.template settle<1>(a, t0, absent, sc);
+    c.template weights<1>(a, sc, p);
     wait_lds();                                        // the keys have been read
-    fetch(a.pool.k, a.pool.ks, t0 + PT_FEW_UNIT, next, kt, true);
+    fetch(true, t0 + PT_FEW_UNIT, next, kt);
     wait_loads<C::FEW_PER>();                          // the values (and `after`) are there
     if (absent || t0 + 32 > q_hi || t0 < q_lo) {
       bool odd = false;
@@ -644,7 +694,7 @@ __device__ __forceinline__ void few(const PtArgs& a, char* lds, int block) {
     }
     c.template add_values<1>(vt, p);
     wait_lds();                                        // the values have been read
-    fetch(a.pool.v, a.pool.vs, t0 + PT_FEW_UNIT, next, vt, false);
+    fetch(false, t0 + PT_FEW_UNIT, next, vt);
     page = next;
     next = page_at(t0 + 2 * PT_FEW_UNIT, after);
   }
@@ -718,42 +768,57 @@ __global__ void __launch_bounds__(PT_THREADS, HD == 256 ? 1 : 2) paged_attn_kern
 }
 
 // Joins the pieces of every row whose keys were cut: one wave per row and head.
+// A row's records are found without its sequence, so the first of them are on
+// their way while the sequence is looked up (a round trip to memory each,
+// three of them one after the other before: 4.4 -> MERGE_US us for one row).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
-  constexpr int E = HD / 64;
+  constexpr int E = HD / 64, AHEAD = 8;
+  typedef float vec __attribute__((ext_vector_type(E)));
   const int lane = threadIdx.x & 63;
-  int64_t rec, orow;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool of_few = (int)blockIdx.x < a.merge_few;
+  const int64_t i = of_few ? (int64_t)blockIdx.x * 4 + wave
+                           : ((int64_t)blockIdx.x - a.merge_few) * 4 + wave;
+  if (!of_few && i >= (int64_t)a.T * a.Hq) return;
+  const int ns = of_few ? a.ns_few : a.ns_many;
+  const int64_t rec = (of_few ? 0 : a.many0) + i * ns;
+  const float2* mls = (const float2*)a.part_ml + rec;
+  const float* sums = a.part + rec * HD + lane * E;
+  // (records past the row's last piece hold anything, and are not used)
+  float2 ml = mls[lane < ns ? lane : 0];
+  vec first[AHEAD];
+#pragma unroll
+  for (int x = 0; x < AHEAD; ++x) first[x] = *(const vec*)(sums + (x < ns ? x : 0) * HD);
+
+  int64_t orow;
   int parts;
-  if ((int)blockIdx.x < a.merge_few) {
-    const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int r = i % PT_FEW, head = i / PT_FEW % a.pool.Hkv, b = i / PT_FEW / a.pool.Hkv;
+  if (of_few) {
+    const int r = (int)(i % PT_FEW), head = (int)(i / PT_FEW) % a.pool.Hkv;
+    const int b = (int)(i / PT_FEW) / a.pool.Hkv;
     const Seq s = sequence(a, b);
     if (!is_few(a, s) || r >= s.n * a.GQ) return;
     parts = span_of(a, s, 0, PT_FEW, PT_FEW_UNIT, a.ns_few).parts;
-    rec = (int64_t)i * a.ns_few;
     const int tok = r / a.GQ;
     orow = (int64_t)(s.first + tok) * a.Hq + head * a.GQ + r - tok * a.GQ;
   } else {
-    orow = ((int64_t)blockIdx.x - a.merge_few) * 4 + (threadIdx.x >> 6);
-    if (orow >= (int64_t)a.T * a.Hq) return;
-    const int row = (int)(orow / a.Hq), head = (int)(orow % a.Hq);
+    orow = i;
+    const int row = (int)(orow / a.Hq), head = (int)(orow - (int64_t)row * a.Hq);
     const int b = sequence_of(a.q_start, a.pool.B, row);
     if (b < 0) return;
     const Seq s = sequence(a, b);
     if (is_few(a, s)) return;
     const int r = (row - s.first) * a.GQ + head % a.GQ;
     parts = span_of(a, s, r / PT_ROWS * PT_ROWS, PT_ROWS, PtCfg<HD>::TN, a.ns_many).parts;
-    rec = a.many0 + orow * a.ns_many;
   }
   if (parts < 2) return;
-  // 64 pieces at a time, one a lane; then their sums, eight loads in flight
-  float top = -INFINITY, l = 0.f, o[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  // 64 pieces at a time, one a lane; then their sums
+  float top = -INFINITY, l = 0.f;
+  vec o = {};
   for (int i0 = 0; i0 < parts; i0 += 64) {
     const int count = min(64, parts - i0);
-    const float2 ml = lane < count ? ((const float2*)a.part_ml)[rec + i0 + lane]
-                                   : make_float2(-INFINITY, 0.f);
+    if (i0) ml = mls[i0 + (lane < count ? lane : 0)];
+    if (lane >= count) ml = make_float2(-INFINITY, 0.f);
     float now = ml.x;
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) now = fmaxf(now, __shfl_xor(now, x));
@@ -765,15 +830,18 @@ __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
     for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
     top = now;
     l = l * old + sum;
+    o *= old;
+    auto factor = [&](int x) {
+      return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), x));
+    };
+    if (i0 == 0) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] *= old;
-    const float* p = a.part + (rec + i0) * HD + lane * E;
-#pragma unroll 8
-    for (int i = 0; i < count; ++i) {
-      const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[e] += fi * p[(int64_t)i * HD + e];
+      for (int x = 0; x < AHEAD; ++x)
+        if (x < count) o += factor(x) * first[x];
     }
+#pragma unroll 8
+    for (int x = i0 ? 0 : AHEAD; x < count; ++x)
+      o += factor(x) * *(const vec*)(sums + (int64_t)(i0 + x) * HD);
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -802,8 +870,11 @@ gsrq_status pt_plan(const gsrq_paged_attn* s, const gsrq_pages* pages, PtPlan& p
   const int64_t Hkv = pages->Hkv, B = pages->B, cap = (int64_t)pages->per * pages->page_size;
   // `few`: pieces for four rounds of two workgroups per CU (lengths differ),
   // of one round of the four waves at the least
+  // (four at the least where the sequences alone would fill it: one of them may
+  // be much longer than the others)
   const int64_t few = std::max<int64_t>(
-      1, std::min((1024 + B * Hkv - 1) / (B * Hkv), (cap + PT_FEW_UNIT - 1) / PT_FEW_UNIT));
+      1, std::min(std::max<int64_t>(4, (1024 + B * Hkv - 1) / (B * Hkv)),
+                  (cap + PT_FEW_UNIT - 1) / PT_FEW_UNIT));
   // `many`: none where no sequence can have more than 32 queries; cut until
   // the launch has two workgroups per CU, into pieces of 512 keys at the least
   p.slots = s->T * GQ > PT_FEW ? s->T * GQ / PT_ROWS + B : 0;

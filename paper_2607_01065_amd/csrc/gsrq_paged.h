@@ -35,7 +35,9 @@ inline gsrq_status page_pool(const gsrq_pages* p, PagePool& o) {
   if ((int64_t)p->page_size * p->per > (1 << 30)) return GSRQ_E_ARG;
   if (p->head_dim != 64 && p->head_dim != 128 && p->head_dim != 256) return GSRQ_E_UNSUPPORTED;
   if (!is_pow2(p->page_size) || p->page_size < 8) return GSRQ_E_UNSUPPORTED;
-  if (p->k_stride[1] >= 1 << 26 || p->v_stride[1] >= 1 << 26) return GSRQ_E_UNSUPPORTED;
+  if (p->k_stride[1] >= 1 << 26 || p->v_stride[1] >= 1 << 26 || p->k_stride[0] > INT32_MAX ||
+      p->v_stride[0] > INT32_MAX)
+    return GSRQ_E_UNSUPPORTED;
   if ((uintptr_t)p->k % 16 || (uintptr_t)p->v % 16) return GSRQ_E_ARG;
   const int count[3] = {p->pages, p->page_size, p->Hkv};
   for (int i = 0; i < 3; ++i) {

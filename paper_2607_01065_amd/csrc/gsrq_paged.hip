@@ -10,8 +10,8 @@
 //
 // Restoring.  A token's row is the sum of its stages' codewords fl32(g s),
 // keys then turned in float32 at the token's position.  A workgroup owns 64
-// dimensions of one head, 32 and the 32 they are turned with, of the keys or
-// of the values: a stage's codewords there are K rows of 256 bytes in LDS.
+// or 128 dimensions of one head, half of them turned with the other half, of the
+// keys or of the values, and holds a stage's codewords there as K rows in LDS.
 #include <algorithm>
 
 #include "gsrq_paged.h"
@@ -148,12 +148,35 @@ struct RestoreArgs {
   int cap, M, G, K, b, d, hd;
 };
 
-__device__ __forceinline__ int code_at(const uint32_t* row, int64_t bit, int b) {
-  const int64_t w = bit >> 5;
-  const int o = (int)(bit & 31);
-  uint32_t v = row[w] >> o;
-  if (o + b > 32) v |= row[w + 1] << (32 - o);
-  return (int)(v & ((1u << b) - 1u));
+// Where a row's code of stage m and subspace g lies.  Codes of 1, 2, 4, 8 or 16
+// bits never cross words; for others the next word, where there is one, comes
+// along.  Reading and extracting are apart so that many codes can be on their
+// way at once, without a branch between them.
+struct CodeBits {
+  int64_t word;
+  int shift;
+};
+template <bool V> struct Bool { static constexpr bool value = V; };
+
+__device__ __forceinline__ CodeBits code_bits(const RestoreArgs& a, int m, int g) {
+  const int64_t bit = ((int64_t)m * a.G + g) * a.b;
+  return {bit >> 5, (int)(bit & 31)};
+}
+// Calls f with whether codes cross words, the same for a whole launch.
+template <typename F> __device__ __forceinline__ void by_crossing(const RestoreArgs& a, F f) {
+  if (32 % a.b) f(Bool<true>());
+  else f(Bool<false>());
+}
+template <bool CROSS>
+__device__ __forceinline__ uint32_t read_code(const RestoreArgs& a, const uint32_t* row,
+                                              const CodeBits& c) {
+  const uint32_t lo = row[c.word];
+  if (!CROSS) return lo;
+  const uint32_t hi = row[c.word + 1 < a.words ? c.word + 1 : c.word];
+  return (uint32_t)(((uint64_t)hi << 32 | lo) >> c.shift);
+}
+__device__ __forceinline__ int code_of(const RestoreArgs& a, uint32_t v, const CodeBits& c) {
+  return (int)(v >> (32 % a.b ? 0 : c.shift) & ((1u << a.b) - 1u));
 }
 
 // Eight elements from element e of a row: the stages' codewords, each rounded
@@ -167,7 +190,11 @@ __device__ __forceinline__ void codeword_sum(const RestoreArgs& a, const uint32_
   for (int j = 0; j < 8; ++j) x[j] = 0.f;
   for (int m = 0; m < a.M; ++m) {
     const int64_t cb = (int64_t)m * a.G + g;
-    const int k = code_at(codes, cb * a.b, a.b);
+    const CodeBits at = code_bits(a, m, g);
+    int k = 0;
+    by_crossing(a, [&](auto cross) {
+      k = code_of(a, read_code<decltype(cross)::value>(a, codes, at), at);
+    });
     const float gk = gain[cb * a.K + k];
     float s[8];
     load8(shape + (cb * a.K + k) * a.d + (e - g * a.d), s);
@@ -176,8 +203,8 @@ __device__ __forceinline__ void codeword_sum(const RestoreArgs& a, const uint32_
   }
 }
 
-// One workgroup's share of a restored cache: 64 dimensions of one head's keys
-// or values.  The slices of one head's codewords stay on one XCD.
+// One workgroup's share of a restored cache: HALF dimensions of one head's keys
+// or values and the HALF they are turned with.
 struct Slice {
   const uint32_t* codes;
   const float *gain, *shape;
@@ -188,17 +215,18 @@ struct Slice {
   int first;                      // of the lower half in the head
 };
 
-template <typename TP>
+template <typename TP, int HALF>
 __device__ __forceinline__ Slice slice_of(const RestoreArgs& a, int sub) {
-  const int slices = a.hd / 64;
+  // (a head's slices 2 Hkv workgroups apart, as a rule on one XCD: its L2
+  // joins their 64-byte pieces of a line)
   const bool key = !(sub & 1);
-  const int slice = (sub >> 1) % slices, head = (sub >> 1) / slices;
+  const int head = (sub >> 1) % a.pool.Hkv, slice = (sub >> 1) / a.pool.Hkv;
   const int64_t* st = key ? a.pool.ks : a.pool.vs;
   Slice s;
   s.codes = key ? a.k_codes : a.v_codes;
   s.gain = key ? a.k_gain : a.v_gain;
   s.shape = key ? a.k_shape : a.v_shape;
-  s.first = 32 * slice;
+  s.first = HALF * slice;
   s.base = (key ? a.pool.k : a.pool.v) + (head * st[2] + s.first) * (int64_t)sizeof(TP);
   s.st0 = st[0] * (int64_t)sizeof(TP);
   s.st1 = st[1] * (int64_t)sizeof(TP);
@@ -225,34 +253,74 @@ __device__ __forceinline__ char* token_at(const RestoreArgs& a, const Slice& s, 
                   : s.base + page * s.st0 + (t & ((1 << a.pool.shift) - 1)) * s.st1;
 }
 
-// All stages' codewords of the slice in LDS (M K 256 bytes), kept while the
-// workgroup goes through chunks of the tokens, its own of the launch's
-// `ranges`.  Four lanes share a token, each with 8 dimensions of the lower half
+// All stages' codewords of the slice in LDS (M K rows of 64 L bytes), kept while
+// the workgroup goes through chunks of the tokens, its own of the launch's
+// `ranges`.  L lanes share a token, each with 8 dimensions of the lower half
 // and the 8 they are turned with: two codes and four 16-byte gathers a stage.
-// The 16 columns of an LDS row are permuted by the codeword's index, so that
-// four tokens' gathers, which all want the same columns, meet in a bank twice
-// and not four times.  Angles: position = chunk + 128 slot + row; the row's
-// rotation stays in registers, the chunk's slots' go through LDS, so that a
-// sine is computed per 128 tokens; c and s carry 15 roundings.
-// Bound by its stores (4 x 32768 tokens x 1024, 1 bit: 0.43 GB).
-constexpr int PR_THREADS = 512;
-constexpr int PR_ROWS = PR_THREADS / 4;
+// L = 8 for heads of 128 and more, so that a workgroup writes whole 128-byte
+// lines (L = 4, 64-byte pieces of a line from two workgroups: 182 us against
+// 129 for 4 x <= 32768 tokens x 1024 of 1 bit, of which 66 without the
+// stores).  The four groups of columns of an LDS row are permuted by the
+// codeword's index, so that tokens' gathers, which want the same columns, meet
+// less in a bank.  Angles: position = chunk + 128 slot + row; the row's rotation
+// stays in registers, the chunk's slots' go through LDS, so that a sine is
+// computed per 128 tokens; c and s carry 15 roundings.
+constexpr int PR_ROWS = 128;
 constexpr int PR_SLOTS = 4;
 constexpr int PR_CHUNK = PR_ROWS * PR_SLOTS;
 constexpr int PR_TABLE = 128 * 1024;        // bytes of codewords, at most
 
-template <typename TP>
-__global__ void __launch_bounds__(PR_THREADS, 4) paged_decode_lds_kernel(RestoreArgs a, int nsub,
-                                                                         int ranges) {
-  extern __shared__ __align__(16) f4 tab[];                 // [M][K][16]
-  __shared__ float2 turns[2][PR_SLOTS][32];
-  const int tid = threadIdx.x, l = tid & 3, rg = tid >> 2;
-  const Slice s = slice_of<TP>(a, blockIdx.x % nsub);
-  const int lo = s.lo + 8 * l, hi = s.hi + 8 * l;
-  for (int i = tid; i < a.M * a.K * 16; i += PR_THREADS) {
-    const int m = i / 16 / a.K, k = i / 16 - m * a.K, c = i & 15;
-    const int q = (c >> 2) ^ (k & 3);                       // lower 0, 1, upper 2, 3
-    tab[i] = codeword4(a, s, m, k, (q < 2 ? s.lo : s.hi) + 8 * (c & 3) + 4 * (q & 1));
+template <typename TP, int M, int L>
+__global__ void __launch_bounds__(PR_ROWS* L, M == 1 ? 4 : 2)
+    paged_decode_lds_kernel(RestoreArgs a, int nsub, int ranges) {
+  constexpr int THREADS = PR_ROWS * L, HALF = 8 * L, COLS = 4 * L;
+  extern __shared__ __align__(16) f4 tab[];                 // [M][K][COLS]
+  __shared__ float2 turns[2][PR_SLOTS][HALF];
+  const int tid = threadIdx.x, l = tid % L, rg = tid / L;
+  const Slice s = slice_of<TP, HALF>(a, blockIdx.x % nsub);
+  const int per = (a.cap + PR_CHUNK - 1) / PR_CHUNK;
+  CodeBits bx[M], by[M];
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    bx[m] = code_bits(a, m, (s.lo + 8 * l) / a.d);
+    by[m] = code_bits(a, m, (s.hi + 8 * l) / a.d);
+  }
+  // the next chunk with tokens from chunk c on, and what it needs from memory,
+  // which is read while the one before is at work: pages and codes (of the
+  // lower and of the upper half)
+  const int64_t end = (int64_t)per * a.pool.B;
+  int64_t c = blockIdx.x / nsub;
+  int next_t0 = 0, next_len = 0, next_entry[PR_SLOTS];
+  uint32_t next_x[PR_SLOTS][M], next_y[PR_SLOTS][M];
+  auto read = [&]() __attribute__((always_inline)) {
+    int b = 0;
+    for (; c < end; c += ranges) {
+      b = (int)(c / per);
+      next_t0 = (int)(c - (int64_t)b * per) * PR_CHUNK;
+      next_len = min(a.seq_len[b], a.cap);
+      if (next_t0 < next_len) break;
+    }
+    if (c >= end) return;
+    const uint32_t* rows = s.codes + ((int64_t)b * a.cap + next_t0) * a.words;
+    by_crossing(a, [&](auto cross) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < PR_SLOTS; ++u) {
+        const int r = min(PR_ROWS * u + rg, next_len - 1 - next_t0);
+        next_entry[u] = entry_of(a.pool, b, next_t0 + r);
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+          next_x[u][m] = read_code<decltype(cross)::value>(a, rows + r * a.words, bx[m]);
+          next_y[u][m] = read_code<decltype(cross)::value>(a, rows + r * a.words, by[m]);
+        }
+      }
+    });
+  };
+  read();
+  if (c >= end) return;
+  for (int i = tid; i < M * a.K * COLS; i += THREADS) {
+    const int m = i / COLS / a.K, k = i / COLS - m * a.K, col = i % COLS;
+    const int q = col / L ^ (k & 3);                        // lower 0, 1, upper 2, 3
+    tab[i] = codeword4(a, s, m, k, (q < 2 ? s.lo : s.hi) + 8 * (col % L) + 4 * (q & 1));
   }
   float cr[8], sr[8];
   if (s.turn) {
@@ -260,39 +328,42 @@ __global__ void __launch_bounds__(PR_THREADS, 4) paged_decode_lds_kernel(Restore
     for (int j = 0; j < 8; ++j) turn_of(rg, a.theta[s.first + 8 * l + j], cr[j], sr[j]);
   }
   __syncthreads();
-  const int per = (a.cap + PR_CHUNK - 1) / PR_CHUNK;
-  int buf = 0;
-  for (int64_t c = blockIdx.x / nsub; c < (int64_t)per * a.pool.B; c += ranges) {
-    const int b = (int)(c / per), t0 = (int)(c - (int64_t)b * per) * PR_CHUNK;
-    const int len = min(a.seq_len[b], a.cap);
-    if (t0 >= len) continue;
+  for (int buf = 0; c < end; buf ^= 1) {
+    const int t0 = next_t0, len = next_len;
+    int entry[PR_SLOTS];
+    uint32_t cx[PR_SLOTS][M], cy[PR_SLOTS][M];
+#pragma unroll
+    for (int u = 0; u < PR_SLOTS; ++u) {
+      entry[u] = next_entry[u];
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        cx[u][m] = next_x[u][m];
+        cy[u][m] = next_y[u][m];
+      }
+    }
     if (s.turn) {
-      if (tid < 32 * PR_SLOTS) {
+      if (tid < HALF * PR_SLOTS) {
         float2 x;
-        turn_of(t0 + PR_ROWS * (tid >> 5), a.theta[s.first + (tid & 31)], x.x, x.y);
-        turns[buf][tid >> 5][tid & 31] = x;
+        turn_of(t0 + PR_ROWS * (tid / HALF), a.theta[s.first + tid % HALF], x.x, x.y);
+        turns[buf][tid / HALF][tid % HALF] = x;
       }
       __syncthreads();
     }
-    int entry[PR_SLOTS];
-#pragma unroll
-    for (int u = 0; u < PR_SLOTS; ++u)
-      entry[u] = entry_of(a.pool, b, min(t0 + PR_ROWS * u + rg, len - 1));
-    const uint32_t* rows = s.codes + ((int64_t)b * a.cap + t0) * a.words;
+    c += ranges;
+    read();
 #pragma unroll
     for (int u = 0; u < PR_SLOTS; ++u) {
       const int t = t0 + PR_ROWS * u + rg;
-      const uint32_t* row = rows + (int64_t)min(PR_ROWS * u + rg, len - 1 - t0) * a.words;
       float x[8], y[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = y[j] = 0.f;
-      for (int m = 0; m < a.M; ++m) {
-        const int kx = code_at(row, ((int64_t)m * a.G + lo / a.d) * a.b, a.b);
-        const int ky = code_at(row, ((int64_t)m * a.G + hi / a.d) * a.b, a.b);
-        const f4* tx = tab + (m * a.K + kx) * 16 + l;
-        const f4* ty = tab + (m * a.K + ky) * 16 + l;
-        const f4 x0 = tx[4 * (kx & 3)], x1 = tx[4 * ((kx & 3) ^ 1)];
-        const f4 y0 = ty[4 * ((ky & 3) ^ 2)], y1 = ty[4 * ((ky & 3) ^ 3)];
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        const int kx = code_of(a, cx[u][m], bx[m]), ky = code_of(a, cy[u][m], by[m]);
+        const f4* tx = tab + (m * a.K + kx) * COLS + l;
+        const f4* ty = tab + (m * a.K + ky) * COLS + l;
+        const f4 x0 = tx[L * (kx & 3)], x1 = tx[L * ((kx & 3) ^ 1)];
+        const f4 y0 = ty[L * ((ky & 3) ^ 2)], y1 = ty[L * ((ky & 3) ^ 3)];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           x[j] += x0[j];
@@ -311,23 +382,25 @@ __global__ void __launch_bounds__(PR_THREADS, 4) paged_decode_lds_kernel(Restore
           y[j] = z * cc + v * ss;
         }
       }
-      char* dst = token_at(a, s, t < len && in_table(a.pool, t) ? checked(a.pool, entry[u]) : -1, t);
+      const bool held = t < len && in_table(a.pool, t);
+      char* dst = token_at(a, s, held ? checked(a.pool, entry[u]) : -1, t);
       if (dst) {
         store8((TP*)dst + 8 * l, x);
         store8((TP*)dst + a.hd / 2 + 8 * l, y);
       }
     }
-    buf ^= 1;
   }
 }
 
 // More stages than LDS holds: a chunk of 64 S tokens keeps its sums in
-// registers and goes through the stages; a stage's codewords are written to
-// one LDS buffer while the tokens gather from the other.  Sixteen lanes share
-// a token, four dimensions each (lanes 0-7 the lower half), so that every
-// gather, whatever the codes, touches every bank once.  SHARED (d >= 32, K <= 256): the
-// eight lanes of a half share a code; each of them holds that of one stage,
-// and two DPP broadcasts hand it out when its turn comes.
+// registers and goes through the stages; a stage's codewords (64 dimensions)
+// are written to one LDS buffer while the tokens gather from the other.
+// Sixteen lanes share a token, four dimensions each (the first eight the lower
+// half), so that a gather touches every bank once, whatever the codes: with
+// eight lanes a token and slices of 32 dimensions the gathers alone took 85 us
+// for 3 x <= 10007 tokens x 1024 of 12 stages.  SHARED (d >= 16): four lanes
+// share a code; each of them holds that of one stage of four, which a DPP
+// broadcast hands out when its turn comes.
 constexpr int PS_THREADS = 1024;
 constexpr int PS_ROWS = PS_THREADS / 16;
 constexpr int PS_K = 256;
@@ -336,28 +409,21 @@ constexpr int PS_BUF = PS_K * 16;           // f4 per buffer
 template <typename TP, int S, bool SHARED>
 __global__ void __launch_bounds__(PS_THREADS) paged_row_decode_stages_kernel(RestoreArgs a,
                                                                              int nsub) {
-  extern __shared__ __align__(16) f4 tab[];                 // [2][PS_BUF]
-  __shared__ float2 turns[S][32];
+  __shared__ __align__(16) f4 tab[2][PS_BUF];
+  __shared__ float2 slot_turn[S][32], row_turn[PS_ROWS][32];
   const int tid = threadIdx.x, l = tid & 15, rg = tid >> 4;
-  const Slice s = slice_of<TP>(a, blockIdx.x % nsub);
   const int per = (a.cap + PS_ROWS * S - 1) / (PS_ROWS * S);
+  const Slice s = slice_of<TP, 32>(a, blockIdx.x % nsub);
   const int chunk = blockIdx.x / nsub;
   const int b = chunk / per, t0 = (chunk - b * per) * PS_ROWS * S;
   const int len = min(a.seq_len[b], a.cap);
   if (t0 >= len) return;
   const int nrows = len - t0;
   const int e = (l < 8 ? s.lo : s.hi - 32) + 4 * l, g = e / a.d;
-  if (s.turn) {
-    for (int i = tid; i < 32 * S; i += PS_THREADS) {
-      float2 x;
-      turn_of(t0 + PS_ROWS * (i >> 5), a.theta[s.first + (i & 31)], x.x, x.y);
-      turns[i >> 5][i & 31] = x;
-    }
-  }
   constexpr int PER = PS_BUF / PS_THREADS;
   f4 v[PER];
   float gk[PER];
-  auto load = [&](int m) {
+  auto load = [&](int m) __attribute__((always_inline)) {
     const float* gb = s.gain + ((int64_t)m * a.G + g) * a.K;
     const float* sb = s.shape + ((int64_t)m * a.G + g) * a.K * a.d + (e - g * a.d);
 #pragma unroll
@@ -367,30 +433,44 @@ __global__ void __launch_bounds__(PS_THREADS) paged_row_decode_stages_kernel(Res
       v[u] = *(const f4*)(sb + k * (uint32_t)a.d);
     }
   };
-  auto store = [&](f4* to) {
-#pragma clang fp contract(off)
-#pragma unroll
-    for (int u = 0; u < PER; ++u) to[u * PS_THREADS + tid] = gk[u] * v[u];
-  };
   f4 acc[S];
 #pragma unroll
   for (int u = 0; u < S; ++u) acc[u] = (f4){0.f, 0.f, 0.f, 0.f};
   int code[S];
   const uint32_t* rows = s.codes + ((int64_t)b * a.cap + t0) * a.words;
   load(0);
+  if (s.turn) {
+    for (int i = tid; i < 32 * (S + PS_ROWS); i += PS_THREADS) {
+      const bool slot = i < 32 * S;
+      const int r = slot ? i >> 5 : (i >> 5) - S;
+      float2 x;
+      turn_of(slot ? t0 + PS_ROWS * r : r, a.theta[s.first + (i & 31)], x.x, x.y);
+      (slot ? slot_turn[r] : row_turn[r])[i & 31] = x;
+    }
+  }
   for (int m = 0; m < a.M; ++m) {
-    f4* from = tab + (m & 1) * PS_BUF;
-    if (!SHARED || (m & 7) == 0) {
+    f4* from = tab[m & 1];
+    if (!SHARED || (m & 3) == 0) {
       // (the row opaque: addresses are formed here, not kept across stages)
       int r = rg;
       asm volatile("" : "+v"(r));
-      const int mm = SHARED ? min(m + (l & 7), a.M - 1) : m;
+      const int mm = SHARED ? min(m + (l & 3), a.M - 1) : m;
       const int64_t bit = ((int64_t)mm * a.G + g) * a.b;
+      const CodeBits at = {bit >> 5, (int)(bit & 31)};
+      by_crossing(a, [&](auto cross) __attribute__((always_inline)) {
 #pragma unroll
-      for (int u = 0; u < S; ++u)
-        code[u] = code_at(rows + (int64_t)min(u * PS_ROWS + r, nrows - 1) * a.words, bit, a.b);
+        for (int u = 0; u < S; ++u)
+          code[u] = (int)read_code<decltype(cross)::value>(
+              a, rows + (int64_t)min(u * PS_ROWS + r, nrows - 1) * a.words, at);
+      });
+#pragma unroll
+      for (int u = 0; u < S; ++u) code[u] = code_of(a, (uint32_t)code[u], at) * 16;
     }
-    store(from);
+    {
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int u = 0; u < PER; ++u) from[u * PS_THREADS + tid] = gk[u] * v[u];
+    }
     if (m + 1 < a.M) load(m + 1);
     // one barrier a stage: who writes stage m + 2 over this buffer has passed
     // stage m + 1's, which all reach only after their gathers of stage m
@@ -399,17 +479,23 @@ __global__ void __launch_bounds__(PS_THREADS) paged_row_decode_stages_kernel(Res
     for (int u = 0; u < S; ++u) {
       int k = code[u];
       if (SHARED) {
-        k = __builtin_amdgcn_update_dpp(k, code[u], 0x150, 0xf, 0x3, false);   // lane 0 to 0-7
-        k = __builtin_amdgcn_update_dpp(k, code[u], 0x158, 0xf, 0xc, false);   // lane 8 to 8-15
-        code[u] = __builtin_amdgcn_update_dpp(0, code[u], 0x12f, 0xf, 0xf, true);
+        k = __builtin_amdgcn_update_dpp(0, code[u], 0x00, 0xf, 0xf, true);        // the quad's first
+        code[u] = __builtin_amdgcn_update_dpp(0, code[u], 0x39, 0xf, 0xf, true);  // and on by one
       }
-      acc[u] += from[k * 16 + l];
+      acc[u] += from[k + l];
     }
   }
+  int entry[S];                           // all read at once
+#pragma unroll
+  for (int u = 0; u < S; ++u) entry[u] = entry_of(a.pool, b, t0 + min(u * PS_ROWS + rg, nrows - 1));
   float cr[4], sr[4];
   if (s.turn) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) turn_of(rg, a.theta[s.first + 4 * (l & 7) + j], cr[j], sr[j]);
+    for (int j = 0; j < 4; ++j) {
+      const float2 w = row_turn[rg][4 * (l & 7) + j];
+      cr[j] = w.x;
+      sr[j] = w.y;
+    }
   }
 #pragma unroll
   for (int u = 0; u < S; ++u) {
@@ -423,13 +509,12 @@ __global__ void __launch_bounds__(PS_THREADS) paged_row_decode_stages_kernel(Res
         // the element that this one is turned with: eight lanes on
         const float z = __uint_as_float(
             __builtin_amdgcn_update_dpp(0u, __float_as_uint(acc[u][j]), 0x128, 0xf, 0xf, true));
-        const float2 w = turns[u][4 * (l & 7) + j];
+        const float2 w = slot_turn[u][4 * (l & 7) + j];
         const float cc = cr[j] * w.x - sr[j] * w.y, ss = sr[j] * w.x + cr[j] * w.y;
         x[j] = x[j] * cc + (l < 8 ? -z : z) * ss;
       }
     }
-    if (t >= len) continue;
-    char* dst = token_at(a, s, page_of(a.pool, b, t), t);
+    char* dst = token_at(a, s, t < len && in_table(a.pool, t) ? checked(a.pool, entry[u]) : -1, t);
     if (!dst) continue;
     typedef TP v4 __attribute__((ext_vector_type(4)));
     v4 r;
@@ -488,46 +573,50 @@ gsrq_status append_launch(const AppendArgs& a, int hd, hipStream_t st) {
   return launch_ok();
 }
 
+template <typename TP, int M, int L>
+gsrq_status restore_resident(const RestoreArgs& a, hipStream_t st) {
+  const int64_t B = a.pool.B, nsub = 2ll * a.pool.Hkv * (a.hd / (16 * L));
+  const int64_t table = (int64_t)M * a.K * 64 * L;
+  // two workgroups per CU where two tables fit, each with its share of the chunks
+  const int64_t chunks = B * ((a.cap + PR_CHUNK - 1) / PR_CHUNK);
+  const int64_t wgs = table <= PR_TABLE / 2 ? 512 : 256;
+  const int64_t ranges = std::max<int64_t>(1, std::min(wgs / nsub, chunks));
+  if (nsub * ranges > (1 << 22) - 1) return GSRQ_E_UNSUPPORTED;   // of up to 1024 threads
+  auto kern = paged_decode_lds_kernel<TP, M, L>;
+  if (table > 65536 - 4096 &&
+      hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize,
+                          (int)table) != hipSuccess)
+    return GSRQ_E_HIP;
+  kern<<<(unsigned)(nsub * ranges), PR_ROWS * L, (size_t)table, st>>>(a, (int)nsub, (int)ranges);
+  return launch_ok();
+}
+
 template <typename TP> gsrq_status restore_launch(const RestoreArgs& a, hipStream_t st) {
   const int64_t B = a.pool.B, nsub = 2ll * a.pool.Hkv * (a.hd / 64);
-  const int64_t table = (int64_t)a.M * a.K * 256;
-  if (table <= PR_TABLE) {
-    // two workgroups per CU where two tables fit, each with its share of the chunks
-    const int64_t chunks = B * ((a.cap + PR_CHUNK - 1) / PR_CHUNK);
-    const int64_t wgs = table <= PR_TABLE / 2 ? 512 : 256;
-    const int64_t ranges = std::max<int64_t>(1, std::min(wgs / nsub, chunks));
-    if (nsub * ranges > MAX_BLOCKS) return GSRQ_E_UNSUPPORTED;
-    auto kern = paged_decode_lds_kernel<TP>;
-    if (table > 65536 - 4096 &&
-        hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize,
-                            (int)table) != hipSuccess)
-      return GSRQ_E_HIP;
-    kern<<<(unsigned)(nsub * ranges), PR_THREADS, (size_t)table, st>>>(a, (int)nsub, (int)ranges);
-    return launch_ok();
+  const int L = a.hd == 64 ? 4 : 8;
+  if (a.M <= (L == 4 ? 2 : 1) && (int64_t)a.M * a.K * 64 * L <= PR_TABLE) {
+    if (L == 8) return restore_resident<TP, 1, 8>(a, st);
+    return a.M == 1 ? restore_resident<TP, 1, 4>(a, st) : restore_resident<TP, 2, 4>(a, st);
   }
   if (a.K <= PS_K) {
-    // chunks of 768 tokens (fewer fills of the stages' buffers) where they
+    // chunks of 640 tokens (fewer fills of the stages' buffers) where they
     // give every CU a workgroup, else of 128
-    constexpr int LONG = 12, SHORT = 2;
+    constexpr int LONG = 10, SHORT = 2;
     const int64_t longs = nsub * B * ((a.cap + PS_ROWS * LONG - 1) / (PS_ROWS * LONG));
     const int64_t shorts = nsub * B * ((a.cap + PS_ROWS * SHORT - 1) / (PS_ROWS * SHORT));
     const bool is_long = longs >= 256;
     const int64_t blocks = is_long ? longs : shorts;
-    if (blocks > (1 << 22) - 1) return GSRQ_E_UNSUPPORTED;   // of 1024 threads
-    const int lds = 2 * PS_BUF * (int)sizeof(f4);
-    auto go = [&](auto kern) -> gsrq_status {
-      if (hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds) !=
-          hipSuccess)
-        return GSRQ_E_HIP;
-      kern<<<(unsigned)blocks, PS_THREADS, lds, st>>>(a, (int)nsub);
-      return launch_ok();
-    };
-    const bool shared = a.d >= 32;
-    if (is_long)
-      return shared ? go(paged_row_decode_stages_kernel<TP, LONG, true>)
-                    : go(paged_row_decode_stages_kernel<TP, LONG, false>);
-    return shared ? go(paged_row_decode_stages_kernel<TP, SHORT, true>)
-                  : go(paged_row_decode_stages_kernel<TP, SHORT, false>);
+    if (blocks > (1 << 22) - 1) return GSRQ_E_UNSUPPORTED;
+    const unsigned n = (unsigned)blocks;
+    const int i = (int)nsub;
+    if (is_long) {
+      if (a.d >= 16) paged_row_decode_stages_kernel<TP, LONG, true><<<n, PS_THREADS, 0, st>>>(a, i);
+      else paged_row_decode_stages_kernel<TP, LONG, false><<<n, PS_THREADS, 0, st>>>(a, i);
+    } else {
+      if (a.d >= 16) paged_row_decode_stages_kernel<TP, SHORT, true><<<n, PS_THREADS, 0, st>>>(a, i);
+      else paged_row_decode_stages_kernel<TP, SHORT, false><<<n, PS_THREADS, 0, st>>>(a, i);
+    }
+    return launch_ok();
   }
   const int64_t items = (int64_t)a.cap * a.pool.Hkv * (a.hd / 16);
   const int64_t blocks = (items + PA_THREADS - 1) / PA_THREADS;

@@ -170,7 +170,8 @@ def _books(M, G, K, d, seed):
     ([25], 30, 2, 256, 32, 2, 5, 8, "f16", True),
     ([1500, 3, 900], 1500, 2, 64, 8, 256, 1, 16, "f16", True),      # several chunks, ranges over sequences
     ([700], 700, 1, 128, 16, 256, 4, 16, "f16", True),              # more stages than LDS holds, codes of their own
-    ([800, 10], 801, 8, 128, 128, 256, 20, 32, "bf16", True),       # past 16 stages, chunks of 768
+    ([800, 10], 801, 8, 128, 128, 256, 20, 32, "bf16", True),       # past 16 stages
+    ([1300, 641, 2600], 2600, 8, 128, 128, 256, 3, 32, "f16", True),  # chunks of 640 tokens
     ([130], 130, 1, 256, 64, 16, 40, 8, "f16", True),               # 4-bit codes, 40 stages
     ([60], 60, 2, 64, 32, 512, 1, 8, "bf16", True),                 # 9-bit codes
 ])

@@ -25,7 +25,7 @@ def _pages(**kw):
 
 BAD_PAGES = [(dict(k=None), 1), (dict(v=PTR + 8), 1), (dict(table=None), 1), (dict(pages=0), 1), (dict(per=0), 1),
              (dict(B=0), 1), (dict(Hkv=0), 1), (dict(ldt=3), 1), (dict(dtype=B.GSRQ_F32), 2), (dict(dtype=9), 1),
-             (dict(page_size=24), 2), (dict(page_size=4), 2), (dict(ks=(1 << 40, 1 << 26, 128)), 2), (dict(page_size=0), 1), (dict(head_dim=96), 2), (dict(head_dim=0), 1),
+             (dict(page_size=24), 2), (dict(page_size=4), 2), (dict(ks=(1 << 30, 1 << 26, 128)), 2), (dict(vs=(1 << 31, 8 * 128, 128)), 2), (dict(page_size=0), 1), (dict(head_dim=96), 2), (dict(head_dim=0), 1),
              (dict(ks=(16 * 8 * 128, 8 * 128 + 4, 128)), 1), (dict(vs=(0, 8 * 128, 128)), 1),
              (dict(per=1 << 20, page_size=1 << 12, ldt=1 << 20), 1)]
 
