@@ -82,7 +82,8 @@ struct PtArgs {
   // [T][Hq][ns_many]
   float *part, *part_ml;
   int64_t many0;                  // first record of the `many` kind
-  int T, Hq, GQ, ns_few, ns_many, window, slots, few_blocks, merge_few;
+  int T, Hq, GQ, ns_few, ns_many, window, slots, first_blocks, merge_few;
+  bool many_first;
   float c;                        // scale * log2(e)
 };
 
@@ -763,26 +764,23 @@ __device__ __forceinline__ void few(const PtArgs& a, char* lds, int block) {
 template <typename T, int HD>
 __global__ void __launch_bounds__(PT_THREADS, HD == 256 ? 1 : 2) paged_attn_kernel(PtArgs a) {
   __shared__ __align__(16) char lds[PtCfg<HD>::LDS];
-  if ((int)blockIdx.x < a.few_blocks) few<T, HD>(a, lds, blockIdx.x);
-  else many<T, HD>(a, lds, blockIdx.x - a.few_blocks);
+  const bool first = (int)blockIdx.x < a.first_blocks;
+  const int block = first ? blockIdx.x : blockIdx.x - a.first_blocks;
+  if (first == a.many_first) many<T, HD>(a, lds, block);
+  else few<T, HD>(a, lds, block);
 }
 
 // Joins the pieces of every row whose keys were cut: one wave per row and head.
 // A row's records are found without its sequence, so the first of them are on
 // their way while the sequence is looked up (a round trip to memory each,
-// three of them one after the other before: 4.4 -> MERGE_US us for one row).
-template <typename T, int HD>
-__global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
-  constexpr int E = HD / 64, AHEAD = 8;
+// three of them one after the other before: 4.4 -> 3.0 us for one token's rows).
+template <typename T, int HD, bool FEW>
+__device__ __forceinline__ void merge(const PtArgs& a, int64_t i) {
+  constexpr int E = HD / 64, AHEAD = FEW ? 8 : 2;
   typedef float vec __attribute__((ext_vector_type(E)));
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const bool of_few = (int)blockIdx.x < a.merge_few;
-  const int64_t i = of_few ? (int64_t)blockIdx.x * 4 + wave
-                           : ((int64_t)blockIdx.x - a.merge_few) * 4 + wave;
-  if (!of_few && i >= (int64_t)a.T * a.Hq) return;
-  const int ns = of_few ? a.ns_few : a.ns_many;
-  const int64_t rec = (of_few ? 0 : a.many0) + i * ns;
+  const int ns = FEW ? a.ns_few : a.ns_many;
+  const int64_t rec = (FEW ? 0 : a.many0) + i * ns;
   const float2* mls = (const float2*)a.part_ml + rec;
   const float* sums = a.part + rec * HD + lane * E;
   // (records past the row's last piece hold anything, and are not used)
@@ -793,7 +791,7 @@ __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
 
   int64_t orow;
   int parts;
-  if (of_few) {
+  if (FEW) {
     const int r = (int)(i % PT_FEW), head = (int)(i / PT_FEW) % a.pool.Hkv;
     const int b = (int)(i / PT_FEW) / a.pool.Hkv;
     const Seq s = sequence(a, b);
@@ -850,6 +848,17 @@ __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
     a.lse[orow] = l == 0.f ? -INFINITY : (top - PT_SHIFT + log2f(l)) * 0.69314718055994531f;
 }
 
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if ((int)blockIdx.x < a.merge_few) {
+    merge<T, HD, true>(a, (int64_t)blockIdx.x * 4 + wave);
+  } else {
+    const int64_t row = ((int64_t)blockIdx.x - a.merge_few) * 4 + wave;
+    if (row < (int64_t)a.T * a.Hq) merge<T, HD, false>(a, row);
+  }
+}
+
 // --------------------------------------------------------------- host side
 
 struct PtPlan {
@@ -876,12 +885,17 @@ gsrq_status pt_plan(const gsrq_paged_attn* s, const gsrq_pages* pages, PtPlan& p
       1, std::min(std::max<int64_t>(4, (1024 + B * Hkv - 1) / (B * Hkv)),
                   (cap + PT_FEW_UNIT - 1) / PT_FEW_UNIT));
   // `many`: none where no sequence can have more than 32 queries; cut until
-  // the launch has two workgroups per CU, into pieces of 512 keys at the least
+  // the launch's tiles (not counting the slots that hold none) give every CU two
+  // workgroups, into pieces of 256 keys at the least, and no more than 1024
+  // workgroups in all (of which those of empty slots, and of sequences that
+  // prove to bring few queries, end at once)
   p.slots = s->T * GQ > PT_FEW ? s->T * GQ / PT_ROWS + B : 0;
   int64_t many = 1;
-  if (p.slots)
-    many = std::max<int64_t>(
-        1, std::min((512 + p.slots * Hkv - 1) / (p.slots * Hkv), (cap + 511) / 512));
+  if (p.slots) {
+    const int64_t tiles = (s->T * GQ + PT_ROWS - 1) / PT_ROWS * Hkv;
+    many = std::min((512 + tiles - 1) / tiles, (cap + 255) / 256);
+    many = std::max<int64_t>(1, std::min(many, 1024 / (p.slots * Hkv)));
+  }
   const int64_t few_blocks = B * Hkv * few, many_blocks = p.slots * Hkv * many;
   const int64_t merge_few = few > 1 ? B * Hkv * (PT_FEW / 4) : 0;
   const int64_t merge_many = p.slots && many > 1 ? (s->T * s->Hq + 3) / 4 : 0;
@@ -951,7 +965,10 @@ gsrq_status gsrq_attn_paged(const gsrq_paged_attn* s, const gsrq_pages* pages,
   a.GQ = s->Hq / pages->Hkv;
   a.ns_few = p.ns_few;
   a.ns_many = p.ns_many;
-  a.few_blocks = p.few_blocks;
+  // the longer workgroups first: those of chunks among single tokens, unless
+  // the sequences bring few rows on average
+  a.many_first = (int64_t)s->T * a.GQ > (int64_t)PT_FEW * pages->B;
+  a.first_blocks = a.many_first ? p.many_blocks : p.few_blocks;
   a.merge_few = p.merge_few;
   a.many0 = p.many0;
   a.window = s->window;
