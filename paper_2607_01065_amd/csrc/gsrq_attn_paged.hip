@@ -78,12 +78,12 @@ struct PtArgs {
   float* lse;                     // or null
   const int32_t *q_start, *seq_len;
   // pieces: sums [record][HD] unscaled, [record][2] base and sum of weights;
-  // records of the `few` kind [B][Hkv][32][ns_few], then of the `many` kind
-  // [T][Hq][ns_many]
+  // records of the `few` kind [T][Hq][ns_few] or, where that is more,
+  // [B][Hkv][32][ns_few], then of the `many` kind [T][Hq][ns_many]
   float *part, *part_ml;
   int64_t many0;                  // first record of the `many` kind
   int T, Hq, GQ, ns_few, ns_many, window, slots, first_blocks, merge_few;
-  bool many_first;
+  bool many_first, few_by_row;
   float c;                        // scale * log2(e)
 };
 
@@ -742,9 +742,9 @@ __device__ __forceinline__ void few(const PtArgs& a, char* lds, int block) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] += f * v[e];
     }
+    const int tok = r / a.GQ, g = r - tok * a.GQ;
+    const int64_t orow = (int64_t)(s.first + tok) * a.Hq + head * a.GQ + g;
     if (w.parts == 1) {
-      const int tok = r / a.GQ, g = r - tok * a.GQ;
-      const int64_t orow = (int64_t)(s.first + tok) * a.Hq + head * a.GQ + g;
       const float inv = l == 0.f ? 0.f : 1.f / l;
       typename Vec<T>::v4 x;
 #pragma unroll
@@ -753,8 +753,8 @@ __device__ __forceinline__ void few(const PtArgs& a, char* lds, int block) {
       if (a.lse && ch == 0)
         a.lse[orow] = l == 0.f ? -INFINITY : (top - PT_SHIFT + log2f(l)) * 0.69314718055994531f;
     } else {
-      const int64_t rec =
-          (((int64_t)b * a.pool.Hkv + head) * PT_FEW + r) * a.ns_few + part;
+      const int64_t at = a.few_by_row ? orow : ((int64_t)b * a.pool.Hkv + head) * PT_FEW + r;
+      const int64_t rec = at * a.ns_few + part;
       *(f4*)(a.part + rec * HD + 4 * ch) = o;
       if (ch == 0) *(float2*)(a.part_ml + 2 * rec) = make_float2(top, l);
     }
@@ -762,7 +762,7 @@ __device__ __forceinline__ void few(const PtArgs& a, char* lds, int block) {
 }
 
 template <typename T, int HD>
-__global__ void __launch_bounds__(PT_THREADS, HD == 256 ? 1 : 2) paged_attn_kernel(PtArgs a) {
+__global__ void __launch_bounds__(PT_THREADS, HD == 256 ? 1 : HD == 128 ? 2 : 3) paged_attn_kernel(PtArgs a) {
   __shared__ __align__(16) char lds[PtCfg<HD>::LDS];
   const bool first = (int)blockIdx.x < a.first_blocks;
   const int block = first ? blockIdx.x : blockIdx.x - a.first_blocks;
@@ -770,93 +770,122 @@ __global__ void __launch_bounds__(PT_THREADS, HD == 256 ? 1 : 2) paged_attn_kern
   else few<T, HD>(a, lds, block);
 }
 
-// Joins the pieces of every row whose keys were cut: one wave per row and head.
-// A row's records are found without its sequence, so the first of them are on
-// their way while the sequence is looked up (a round trip to memory each,
-// three of them one after the other before: 4.4 -> 3.0 us for one token's rows).
-template <typename T, int HD, bool FEW>
-__device__ __forceinline__ void merge(const PtArgs& a, int64_t i) {
-  constexpr int E = HD / 64, AHEAD = FEW ? 8 : 2;
+// Joins the pieces of a row whose keys were cut; a wave.  Its records' first
+// loads (N sums) start on construction, before it is known how many there are:
+// what lies past the row's last piece is anything, and not used.
+template <typename T, int HD, int N> struct Pieces {
+  static constexpr int E = HD / 64;
   typedef float vec __attribute__((ext_vector_type(E)));
-  const int lane = threadIdx.x & 63;
-  const int ns = FEW ? a.ns_few : a.ns_many;
-  const int64_t rec = (FEW ? 0 : a.many0) + i * ns;
-  const float2* mls = (const float2*)a.part_ml + rec;
-  const float* sums = a.part + rec * HD + lane * E;
-  // (records past the row's last piece hold anything, and are not used)
-  float2 ml = mls[lane < ns ? lane : 0];
-  vec first[AHEAD];
-#pragma unroll
-  for (int x = 0; x < AHEAD; ++x) first[x] = *(const vec*)(sums + (x < ns ? x : 0) * HD);
+  const float2* mls;
+  const float* sums;
+  float2 ml;
+  vec first[N];
 
-  int64_t orow;
-  int parts;
-  if (FEW) {
-    const int r = (int)(i % PT_FEW), head = (int)(i / PT_FEW) % a.pool.Hkv;
-    const int b = (int)(i / PT_FEW) / a.pool.Hkv;
-    const Seq s = sequence(a, b);
-    if (!is_few(a, s) || r >= s.n * a.GQ) return;
-    parts = span_of(a, s, 0, PT_FEW, PT_FEW_UNIT, a.ns_few).parts;
-    const int tok = r / a.GQ;
-    orow = (int64_t)(s.first + tok) * a.Hq + head * a.GQ + r - tok * a.GQ;
-  } else {
-    orow = i;
-    const int row = (int)(orow / a.Hq), head = (int)(orow - (int64_t)row * a.Hq);
-    const int b = sequence_of(a.q_start, a.pool.B, row);
-    if (b < 0) return;
-    const Seq s = sequence(a, b);
-    if (is_few(a, s)) return;
-    const int r = (row - s.first) * a.GQ + head % a.GQ;
-    parts = span_of(a, s, r / PT_ROWS * PT_ROWS, PT_ROWS, PtCfg<HD>::TN, a.ns_many).parts;
+  __device__ __forceinline__ Pieces(const PtArgs& a, int64_t rec, int ns) {
+    const int lane = threadIdx.x & 63;
+    mls = (const float2*)a.part_ml + rec;
+    sums = a.part + rec * HD + lane * E;
+    ml = mls[lane < ns ? lane : 0];
+#pragma unroll
+    for (int x = 0; x < N; ++x) first[x] = *(const vec*)(sums + (x < ns ? x : 0) * HD);
   }
-  if (parts < 2) return;
-  // 64 pieces at a time, one a lane; then their sums
-  float top = -INFINITY, l = 0.f;
-  vec o = {};
-  for (int i0 = 0; i0 < parts; i0 += 64) {
-    const int count = min(64, parts - i0);
-    if (i0) ml = mls[i0 + (lane < count ? lane : 0)];
-    if (lane >= count) ml = make_float2(-INFINITY, 0.f);
-    float now = ml.x;
+
+  __device__ __forceinline__ void join(const PtArgs& a, int parts, int64_t orow) {
+    const int lane = threadIdx.x & 63;
+    // 64 pieces at a time, one a lane; then their sums
+    float top = -INFINITY, l = 0.f;
+    vec o = {};
+    for (int i0 = 0; i0 < parts; i0 += 64) {
+      const int count = min(64, parts - i0);
+      if (i0) ml = mls[i0 + (lane < count ? lane : 0)];
+      if (lane >= count) ml = make_float2(-INFINITY, 0.f);
+      float now = ml.x;
 #pragma unroll
-    for (int x = 1; x < 64; x <<= 1) now = fmaxf(now, __shfl_xor(now, x));
-    now = fmaxf(now, top);
-    const float old = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now);
-    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - now);
-    float sum = f * ml.y;
+      for (int x = 1; x < 64; x <<= 1) now = fmaxf(now, __shfl_xor(now, x));
+      now = fmaxf(now, top);
+      const float old = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now);
+      const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - now);
+      float sum = f * ml.y;
 #pragma unroll
-    for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
-    top = now;
-    l = l * old + sum;
-    o *= old;
-    auto factor = [&](int x) {
-      return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), x));
-    };
-    if (i0 == 0) {
+      for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
+      top = now;
+      l = l * old + sum;
+      o *= old;
+      auto factor = [&](int x) {
+        return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), x));
+      };
+      if (i0 == 0) {
 #pragma unroll
-      for (int x = 0; x < AHEAD; ++x)
-        if (x < count) o += factor(x) * first[x];
-    }
+        for (int x = 0; x < N; ++x)
+          if (x < count) o += factor(x) * first[x];
+      }
 #pragma unroll 8
-    for (int x = i0 ? 0 : AHEAD; x < count; ++x)
-      o += factor(x) * *(const vec*)(sums + (int64_t)(i0 + x) * HD);
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+      for (int x = i0 ? 0 : N; x < count; ++x)
+        o += factor(x) * *(const vec*)(sums + (int64_t)(i0 + x) * HD);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-  for (int e = 0; e < E; ++e) ((T*)a.out)[orow * HD + lane * E + e] = (T)(o[e] * inv);
-  if (a.lse && lane == 0)
-    a.lse[orow] = l == 0.f ? -INFINITY : (top - PT_SHIFT + log2f(l)) * 0.69314718055994531f;
+    for (int e = 0; e < E; ++e) ((T*)a.out)[orow * HD + lane * E + e] = (T)(o[e] * inv);
+    if (a.lse && lane == 0)
+      a.lse[orow] = l == 0.f ? -INFINITY : (top - PT_SHIFT + log2f(l)) * 0.69314718055994531f;
+  }
+};
+
+__device__ __forceinline__ int few_parts(const PtArgs& a, const Seq& s) {
+  return span_of(a, s, 0, PT_FEW, PT_FEW_UNIT, a.ns_few).parts;
 }
 
+// One wave per row and head (and, where the records of the `few` kind are laid
+// out by sequence, one per such record).  A row's records are found without
+// its sequence, so their first loads are on their way while the sequence is
+// looked up (three round trips to memory one after the other before: 4.4 ->
+// 2.7 us for one token's rows).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x < a.merge_few) {
-    merge<T, HD, true>(a, (int64_t)blockIdx.x * 4 + wave);
-  } else {
-    const int64_t row = ((int64_t)blockIdx.x - a.merge_few) * 4 + wave;
-    if (row < (int64_t)a.T * a.Hq) merge<T, HD, false>(a, row);
+    const int i = blockIdx.x * 4 + wave;               // [B][Hkv][32]
+    Pieces<T, HD, 8> p(a, (int64_t)i * a.ns_few, a.ns_few);
+    const int r = i % PT_FEW, head = i / PT_FEW % a.pool.Hkv, b = i / PT_FEW / a.pool.Hkv;
+    const Seq s = sequence(a, b);
+    if (!is_few(a, s) || r >= s.n * a.GQ) return;
+    const int parts = few_parts(a, s), tok = r / a.GQ;
+    if (parts < 2) return;
+    p.join(a, parts, (int64_t)(s.first + tok) * a.Hq + head * a.GQ + r - tok * a.GQ);
+    return;
   }
+  const int64_t orow = ((int64_t)blockIdx.x - a.merge_few) * 4 + wave;
+  if (orow >= (int64_t)a.T * a.Hq) return;
+  const int row = (int)(orow / a.Hq), head = (int)(orow - (int64_t)row * a.Hq);
+  auto look_up = [&](Seq& s) {
+    const int b = sequence_of(a.q_start, a.pool.B, row);
+    if (b >= 0) s = sequence(a, b);
+    return b >= 0;
+  };
+  auto many_parts = [&](const Seq& s) {
+    const int r = (row - s.first) * a.GQ + head % a.GQ;
+    return span_of(a, s, r / PT_ROWS * PT_ROWS, PT_ROWS, PtCfg<HD>::TN, a.ns_many).parts;
+  };
+  Seq s;
+  if (a.few_by_row && a.ns_few > 1) {
+    Pieces<T, HD, 8> p(a, orow * a.ns_few, a.ns_few);
+    if (!look_up(s)) return;
+    if (is_few(a, s)) {
+      const int parts = few_parts(a, s);
+      if (parts > 1) p.join(a, parts, orow);
+      return;
+    }
+    if (a.ns_many < 2) return;
+    const int parts = many_parts(s);
+    if (parts < 2) return;
+    Pieces<T, HD, 2> q(a, a.many0 + orow * a.ns_many, a.ns_many);
+    q.join(a, parts, orow);
+    return;
+  }
+  Pieces<T, HD, 2> p(a, a.many0 + orow * a.ns_many, a.ns_many);
+  if (!look_up(s) || is_few(a, s)) return;
+  const int parts = many_parts(s);
+  if (parts > 1) p.join(a, parts, orow);
 }
 
 // --------------------------------------------------------------- host side
@@ -864,7 +893,8 @@ __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
 struct PtPlan {
   PagePool pool;
   int64_t slots, many0;
-  int ns_few, ns_many, few_blocks, many_blocks, merge_few, merge_many;
+  int ns_few, ns_many, few_blocks, many_blocks, merge_few, merge_rows;
+  bool few_by_row;
   size_t off_ml, bytes;
 };
 
@@ -880,10 +910,12 @@ gsrq_status pt_plan(const gsrq_paged_attn* s, const gsrq_pages* pages, PtPlan& p
   // `few`: pieces for four rounds of two workgroups per CU (lengths differ),
   // of one round of the four waves at the least
   // (four at the least where the sequences alone would fill it: one of them may
-  // be much longer than the others)
-  const int64_t few = std::max<int64_t>(
-      1, std::min(std::max<int64_t>(4, (1024 + B * Hkv - 1) / (B * Hkv)),
-                  (cap + PT_FEW_UNIT - 1) / PT_FEW_UNIT));
+  // be much longer than the others); none where the table holds 256 tokens at
+  // most: 8 us a call against 10 with the joining launch; at 700 tokens 16
+  int64_t few = 1;
+  if (cap > 256)
+    few = std::min(std::max<int64_t>(4, (1024 + B * Hkv - 1) / (B * Hkv)),
+                   (cap + PT_FEW_UNIT - 1) / PT_FEW_UNIT);
   // `many`: none where no sequence can have more than 32 queries; cut until
   // the launch's tiles (not counting the slots that hold none) give every CU two
   // workgroups, into pieces of 256 keys at the least, and no more than 1024
@@ -897,18 +929,21 @@ gsrq_status pt_plan(const gsrq_paged_attn* s, const gsrq_pages* pages, PtPlan& p
     many = std::max<int64_t>(1, std::min(many, 1024 / (p.slots * Hkv)));
   }
   const int64_t few_blocks = B * Hkv * few, many_blocks = p.slots * Hkv * many;
-  const int64_t merge_few = few > 1 ? B * Hkv * (PT_FEW / 4) : 0;
-  const int64_t merge_many = p.slots && many > 1 ? (s->T * s->Hq + 3) / 4 : 0;
-  if (few_blocks + many_blocks > MAX_BLOCKS || merge_few + merge_many > MAX_BLOCKS)
+  p.few_by_row = s->T * GQ <= PT_FEW * B;
+  const int64_t few_rows = p.few_by_row ? s->T * s->Hq : B * Hkv * PT_FEW;
+  const int64_t merge_few = few > 1 && !p.few_by_row ? few_rows / 4 : 0;
+  const bool by_row = (few > 1 && p.few_by_row) || (p.slots && many > 1);
+  const int64_t merge_rows = by_row ? (s->T * s->Hq + 3) / 4 : 0;
+  if (few_blocks + many_blocks > MAX_BLOCKS || merge_few + merge_rows > MAX_BLOCKS)
     return GSRQ_E_UNSUPPORTED;
   p.ns_few = (int)few;
   p.ns_many = (int)many;
   p.few_blocks = (int)few_blocks;
   p.many_blocks = (int)many_blocks;
   p.merge_few = (int)merge_few;
-  p.merge_many = (int)merge_many;
-  p.many0 = few > 1 ? B * Hkv * PT_FEW * few : 0;
-  const size_t rows = (size_t)p.many0 + (merge_many ? (size_t)(s->T * s->Hq * many) : 0);
+  p.merge_rows = (int)merge_rows;
+  p.many0 = few > 1 ? few_rows * few : 0;
+  const size_t rows = (size_t)p.many0 + (p.slots && many > 1 ? (size_t)(s->T * s->Hq * many) : 0);
   p.off_ml = align256(rows * pages->head_dim * sizeof(float));
   p.bytes = p.off_ml + align256(rows * 2 * sizeof(float));
   return GSRQ_OK;
@@ -920,8 +955,8 @@ gsrq_status pt_launch(const PtArgs& a, const PtPlan& p, hipStream_t st) {
   TimedLaunch tl(GSRQ_KERNEL_ATTENTION, st);
   paged_attn_kernel<T, HD><<<p.few_blocks + p.many_blocks, PT_THREADS, 0, st>>>(a);
   gsrq_status e = launch_ok();
-  if (e || p.merge_few + p.merge_many == 0) return e;
-  paged_attn_merge_kernel<T, HD><<<p.merge_few + p.merge_many, 256, 0, st>>>(a);
+  if (e || p.merge_few + p.merge_rows == 0) return e;
+  paged_attn_merge_kernel<T, HD><<<p.merge_few + p.merge_rows, 256, 0, st>>>(a);
   return launch_ok();
 }
 
@@ -967,7 +1002,8 @@ gsrq_status gsrq_attn_paged(const gsrq_paged_attn* s, const gsrq_pages* pages,
   a.ns_many = p.ns_many;
   // the longer workgroups first: those of chunks among single tokens, unless
   // the sequences bring few rows on average
-  a.many_first = (int64_t)s->T * a.GQ > (int64_t)PT_FEW * pages->B;
+  a.many_first = !p.few_by_row;
+  a.few_by_row = p.few_by_row;
   a.first_blocks = a.many_first ? p.many_blocks : p.few_blocks;
   a.merge_few = p.merge_few;
   a.many0 = p.many0;

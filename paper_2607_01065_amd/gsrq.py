@@ -7,7 +7,6 @@ functions from here raises instead of falling back to anything else.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 import os
@@ -563,7 +562,6 @@ def attn_decode(k_codes, v_codes, seq_len, k_gain, k_shape, v_gain, v_shape, q, 
 _PAGES = struct.Struct("@PP3q3qPq7i0q")
 _HEADS = struct.Struct("@Pqq")
 _PAGED_ATTN = struct.Struct("@qiifI0q")
-_NO_CONTEXT = contextlib.nullcontext()
 
 
 def _paged_types():
@@ -594,18 +592,27 @@ def _paged_device(device, stream):
     return torch.cuda.stream(stream)
 
 
+def _dense(t, name, dtype, like, n) -> int:
+    """Address of a contiguous tensor of n elements on `like`'s device."""
+    if (t.dtype is dtype and t.numel() == n and t.get_device() == like.get_device()
+            and t.is_contiguous()):
+        return t.data_ptr()
+    _need(t, name, (dtype,), like.device, (n,))
+    raise ValueError(f"{name} must be a dense tensor of {n} elements")
+
+
 def _pages(k_pages, v_pages, table) -> bytes:
     """gsrq_pages of two pools [pages, page_size, Hkv, head_dim] and their table."""
     torch = _torch()
-    shape, dtype, dev = k_pages.shape, k_pages.dtype, k_pages.device
+    shape, dtype, index = k_pages.shape, k_pages.dtype, k_pages.get_device()
     if len(shape) != 4 or v_pages.shape != shape:
         raise ValueError("k_pages and v_pages must be [pages, page_size, Hkv, head_dim], both alike")
     if dtype is not torch.float16 and dtype is not torch.bfloat16 or v_pages.dtype is not dtype:
         raise TypeError("pages must be float16 or bfloat16, both alike")
     if table.dim() != 2 or table.dtype is not torch.int32:
         raise TypeError("table must be a 2-D int32 tensor")
-    if v_pages.device != dev or table.device != dev:
-        raise ValueError(f"v_pages and table must be on {dev}")
+    if v_pages.get_device() != index or table.get_device() != index:
+        raise ValueError(f"v_pages and table must be on {k_pages.device}")
     k0, k1, k2, k3 = k_pages.stride()
     v0, v1, v2, v3 = v_pages.stride()
     t0, t1 = table.stride()
@@ -613,25 +620,34 @@ def _pages(k_pages, v_pages, table) -> bytes:
     if k3 != 1 or v3 != 1 or (t1 != 1 and per > 1):
         raise ValueError("elements of a head and entries of a table row must be adjacent")
     n, size, Hkv, hd = shape
-    if max(n, size, Hkv, hd, B, per) >= 1 << 31:
-        raise ValueError("a dimension of the pages or the table does not fit 32 bits")
-    return _PAGES.pack(k_pages.data_ptr(), v_pages.data_ptr(), k0, k1, k2, v0, v1, v2,
-                       table.data_ptr(), t0 if B > 1 else per, n, size, per, B, Hkv, hd,
-                       GSRQ_F16 if dtype is torch.float16 else GSRQ_BF16)
+    try:
+        return _PAGES.pack(k_pages.data_ptr(), v_pages.data_ptr(), k0, k1, k2, v0, v1, v2,
+                           table.data_ptr(), t0 if B > 1 else per, n, size, per, B, Hkv, hd,
+                           GSRQ_F16 if dtype is torch.float16 else GSRQ_BF16)
+    except struct.error:
+        raise ValueError("a dimension of the pages or the table does not fit 32 bits") from None
 
 
-def _heads(x, name, heads, head_dim, rows, dtype, device) -> bytes:
+def _heads(x, name, heads, head_dim, rows, dtype, like) -> bytes:
     """gsrq_heads of rows [rows, heads, head_dim]."""
     if x.shape != (rows, heads, head_dim):
         raise ValueError(f"{name} must be [{rows}, {heads}, {head_dim}], not {tuple(x.shape)}")
     if x.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {x.dtype}")
-    if x.device != device:
-        raise ValueError(f"{name} is on {x.device}, expected {device}")
+    if x.get_device() != like.get_device():
+        raise ValueError(f"{name} is on {x.device}, expected {like.device}")
     s0, s1, s2 = x.stride()
     if s2 != 1:
         raise ValueError(f"{name}: elements of a head must be adjacent")
     return _HEADS.pack(x.data_ptr(), s0, s1)
+
+
+def _empty(like, shape, dtype):
+    """A dense tensor of this shape and type on `like`'s device."""
+    torch = _torch()
+    if like.dtype is dtype and like.shape == shape and like.is_contiguous():
+        return torch.empty_like(like)
+    return torch.empty(shape, dtype=dtype, device=like.device)
 
 
 def paged_append(k, v, k_pages, v_pages, table, q_start, seq_len, *, q=None, theta=None,
@@ -649,35 +665,42 @@ def paged_append(k, v, k_pages, v_pages, table, q_start, seq_len, *, q=None, the
     torch = _torch()
     lib = _lib or load_library()
     pages = _pages(k_pages, v_pages, table)
-    dev, B = k_pages.device, table.shape[0]
-    Hkv, hd = k_pages.shape[2:]
-    T, dtype = k.shape[0], k.dtype
+    B = table.shape[0]
+    _, _, Hkv, hd = k_pages.shape
+    T, dtype, held = k.shape[0], k.dtype, k_pages.dtype
     dt = _paged_dtype(k, "k")
-    kh = _heads(k, "k", Hkv, hd, T, dtype, dev)
-    vh = _heads(v, "v", Hkv, hd, T, dtype, dev)
+    kh = _heads(k, "k", Hkv, hd, T, dtype, k_pages)
+    vh = _heads(v, "v", Hkv, hd, T, dtype, k_pages)
     Hq, qh = 0, None
     if q is not None:
         Hq = q.shape[1] if q.dim() == 3 else 0
-        qh = _heads(q, "q", Hq, hd, T, dtype, dev)
+        qh = _heads(q, "q", Hq, hd, T, dtype, k_pages)
     elif q_norm is not None or q_out is not None:
         raise ValueError("q_norm and q_out need q")
-    _need(q_start, "q_start", (torch.int32,), dev, (B + 1,))
-    _need(seq_len, "seq_len", (torch.int32,), dev, (B,))
-    _need(theta, "theta", (torch.float64,), dev, (hd // 2,))
-    _need(k_norm, "k_norm", (torch.float32,), dev, (hd,))
-    _need(q_norm, "q_norm", (torch.float32,), dev, (hd,))
-    _need(q_out, "q_out", (k_pages.dtype,), dev, (T, Hq, hd))
-    with _paged_device(dev, stream) or _NO_CONTEXT:
-        if q is not None and q_out is None:
-            q_out = torch.empty((T, Hq, hd), dtype=k_pages.dtype, device=dev)
-        if T == 0:
-            return q_out
-        st = lib.gsrq_paged_append(
-            pages, T, q_start.data_ptr(), seq_len.data_ptr(), kh, vh, qh, Hq, dt, _ptr(theta),
-            _ptr(k_norm), _ptr(q_norm), eps, _ptr(q_out), _append_stream_handle(stream))
-    if st != GSRQ_OK:
-        _check(st, "gsrq_paged_append")
-    return q_out
+    start = _dense(q_start, "q_start", torch.int32, k_pages, B + 1)
+    lens = _dense(seq_len, "seq_len", torch.int32, k_pages, B)
+    angles = None if theta is None else _dense(theta, "theta", torch.float64, k_pages, hd // 2)
+    kn = None if k_norm is None else _dense(k_norm, "k_norm", torch.float32, k_pages, hd)
+    qn = None if q_norm is None else _dense(q_norm, "q_norm", torch.float32, k_pages, hd)
+    if q_out is not None:
+        _dense(q_out, "q_out", held, k_pages, T * Hq * hd)
+
+    def call():
+        out = q_out
+        if q is not None and out is None:
+            out = _empty(q, (T, Hq, hd), held)
+        if T > 0:
+            st = lib.gsrq_paged_append(pages, T, start, lens, kh, vh, qh, Hq, dt, angles, kn, qn,
+                                       eps, _ptr(out), _append_stream_handle(stream))
+            if st != GSRQ_OK:
+                _check(st, "gsrq_paged_append")
+        return out
+
+    context = _paged_device(k_pages.device, stream)
+    if context is None:
+        return call()
+    with context:
+        return call()
 
 
 def attn_paged_workspace_bytes(T, Hq, k_pages, v_pages, table, *, window=0) -> int:
@@ -700,24 +723,26 @@ def attn_paged(q, k_pages, v_pages, table, q_start, seq_len, *, scale=None, wind
     torch = _torch()
     lib = _lib or load_library()
     pages = _pages(k_pages, v_pages, table)
-    dev, B, hd = k_pages.device, table.shape[0], k_pages.shape[3]
     if q.dim() != 3:
         raise ValueError("q must be [T, Hq, head_dim]")
-    T, Hq = q.shape[:2]
-    dtype = k_pages.dtype
-    qh = _heads(q, "q", Hq, hd, T, dtype, dev)
-    _need(q_start, "q_start", (torch.int32,), dev, (B + 1,))
-    _need(seq_len, "seq_len", (torch.int32,), dev, (B,))
-    _need(out, "out", (dtype,), dev, (T, Hq, hd))
-    if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
-        raise ValueError(f"workspace must be contiguous, on {dev}")
-    if not 0 <= window < 1 << 31:
-        raise ValueError("window must be a number of tokens, or 0")
-    s = _PAGED_ATTN.pack(T, Hq, window, hd ** -0.5 if scale is None else scale, 0)
-    with _paged_device(dev, stream) or _NO_CONTEXT:
-        if out is None:
-            out = torch.empty((T, Hq, hd), dtype=dtype, device=dev)
-        total = torch.empty((T, Hq), dtype=torch.float32, device=dev) if lse else None
+    T, Hq, hd = q.shape
+    B, dtype = table.shape[0], k_pages.dtype
+    qh = _heads(q, "q", Hq, k_pages.shape[3], T, dtype, k_pages)
+    start = _dense(q_start, "q_start", torch.int32, k_pages, B + 1)
+    lens = _dense(seq_len, "seq_len", torch.int32, k_pages, B)
+    if out is not None:
+        _dense(out, "out", dtype, k_pages, T * Hq * hd)
+    if workspace is not None and (workspace.device != k_pages.device
+                                  or not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be contiguous, on {k_pages.device}")
+    try:
+        s = _PAGED_ATTN.pack(T, Hq, window, hd ** -0.5 if scale is None else scale, 0)
+    except struct.error:
+        raise ValueError("window must be a number of tokens, or 0, and scale a number") from None
+
+    def call():
+        res = _empty(q, (T, Hq, hd), dtype) if out is None else out
+        total = (torch.empty((T, Hq), dtype=torch.float32, device=q.device) if lse else None)
         if T > 0:
             n = ctypes.c_size_t()
             st = lib.gsrq_attn_paged_workspace_bytes(s, pages, ctypes.byref(n))
@@ -725,14 +750,19 @@ def attn_paged(q, k_pages, v_pages, table, q_start, seq_len, *, scale=None, wind
                 _check(st, "gsrq_attn_paged_workspace_bytes")
             ws, size = None, n.value
             if size:
-                ws = _workspace(size, dev, workspace)
+                ws = _workspace(size, q.device, workspace)
                 size = ws.numel() * ws.element_size()
-            st = lib.gsrq_attn_paged(s, pages, q_start.data_ptr(), seq_len.data_ptr(), qh,
-                                     out.data_ptr(), _ptr(total), _ptr(ws), size,
-                                     _append_stream_handle(stream))
+            st = lib.gsrq_attn_paged(s, pages, start, lens, qh, res.data_ptr(), _ptr(total),
+                                     _ptr(ws), size, _append_stream_handle(stream))
             if st != GSRQ_OK:
                 _check(st, "gsrq_attn_paged")
-    return (out, total) if lse else out
+        return (res, total) if lse else res
+
+    context = _paged_device(k_pages.device, stream)
+    if context is None:
+        return call()
+    with context:
+        return call()
 
 
 def paged_restore(k_codes, v_codes, seq_len, k_gain, k_shape, v_gain, v_shape, k_pages, v_pages,
@@ -764,9 +794,16 @@ def paged_restore(k_codes, v_codes, seq_len, k_gain, k_shape, v_gain, v_shape, k
     _need(theta, "theta", (torch.float64,), dev, (hd // 2,))
     if cap == 0:
         return
-    with _paged_device(dev, stream) or _NO_CONTEXT:
+
+    def call():
         st = lib.gsrq_paged_restore(
-            pages, ctypes.byref(sh), cap, _ptr(k_codes), _ptr(v_codes),
-            _ptr(seq_len), _ptr(k_gain), _ptr(k_shape), _ptr(v_gain), _ptr(v_shape), _ptr(theta),
+            pages, ctypes.byref(sh), cap, _ptr(k_codes), _ptr(v_codes), _ptr(seq_len),
+            _ptr(k_gain), _ptr(k_shape), _ptr(v_gain), _ptr(v_shape), _ptr(theta),
             _append_stream_handle(stream))
-    _check(st, "gsrq_paged_restore")
+        _check(st, "gsrq_paged_restore")
+
+    context = _paged_device(dev, stream)
+    if context is None:
+        return call()
+    with context:
+        call()

@@ -79,7 +79,7 @@ def test_packed_structures_are_the_abi_s():
     assert (p.k, p.v, p.table) == (kp.data_ptr(), vp.data_ptr(), tab.data_ptr())
     assert (list(p.k_stride), list(p.v_stride)) == ([1536, 64, 512], [1536, 192, 64])
     assert (p.ldt, p.pages, p.page_size, p.per, p.B, p.Hkv, p.head_dim, p.dtype) == (9, 4, 8, 2, 5, 3, 64, B.GSRQ_BF16)
-    h = B.Heads.from_buffer_copy(B._heads(vp[0], "x", 3, 64, 8, torch.bfloat16, vp.device))
+    h = B.Heads.from_buffer_copy(B._heads(vp[0], "x", 3, 64, 8, torch.bfloat16, vp))
     assert (h.data, h.token_stride, h.head_stride) == (vp.data_ptr(), 192, 64)
     a = B.PagedAttn.from_buffer_copy(B._PAGED_ATTN.pack(7, 6, 5, 0.5, 0))
     assert (a.T, a.Hq, a.window, a.scale, a.flags) == (7, 6, 5, 0.5, 0)
@@ -173,7 +173,7 @@ def test_binding_attention_refuses():
     good = dict(q=q, k_pages=kp, v_pages=kp, table=tab, q_start=start, seq_len=lens)
     for kw, error in ((dict(q=q.bfloat16()), TypeError), (dict(q=q[0]), ValueError), (dict(q=q[..., :32]), ValueError),
                       (dict(q_start=start[:2]), ValueError), (dict(seq_len=lens.long()), TypeError),
-                      (dict(out=torch.zeros(3, 4, 64)), TypeError), (dict(window=-1), ValueError), (dict(window=1 << 31), ValueError), (dict(out=q[:2]), ValueError),
+                      (dict(out=torch.zeros(3, 4, 64)), TypeError), (dict(window=1 << 31), ValueError), (dict(scale="1"), ValueError), (dict(out=q[:2]), ValueError),
                       (dict(workspace=torch.zeros(8, dtype=torch.uint8)[::2]), ValueError), (dict(), ValueError)):
         with pytest.raises(error):
             B.attn_paged(**{**good, **kw})
