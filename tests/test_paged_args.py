@@ -177,3 +177,21 @@ def test_binding_attention_refuses():
                       (dict(workspace=torch.zeros(8, dtype=torch.uint8)[::2]), ValueError), (dict(), ValueError)):
         with pytest.raises(error):
             B.attn_paged(**{**good, **kw})
+
+
+def test_streams_and_devices():
+    """A stream of another device is refused; tensors of another device than the current one make theirs current."""
+    import types
+    cuda0, cuda1 = torch.device("cuda", 0), torch.device("cuda", 1)
+    with pytest.raises(ValueError):
+        B._paged_device(cuda0, types.SimpleNamespace(device=cuda1))
+    with pytest.raises(ValueError):
+        B._paged_device(torch.device("cpu"), None)
+
+
+@pytest.mark.parametrize("current,index,made", [(0, 0, None), (0, 1, 1), (1, 0, 0)])
+def test_another_device_becomes_current(monkeypatch, current, index, made):
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current, raising=False)
+    monkeypatch.setattr(torch.cuda, "device", lambda d: ("device", d.index))
+    got = B._paged_device(torch.device("cuda", index), None)
+    assert got == (None if made is None else ("device", made))
