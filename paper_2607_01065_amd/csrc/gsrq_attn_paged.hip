@@ -83,7 +83,7 @@ struct PtArgs {
   float *part, *part_ml;
   int64_t many0;                  // first record of the `many` kind
   int T, Hq, GQ, ns_few, ns_many, window, slots, first_blocks, merge_few;
-  bool many_first, few_by_row;
+  bool many_first, few_by_row, merge_shared;
   float c;                        // scale * log2(e)
 };
 
@@ -638,46 +638,61 @@ __device__ __forceinline__ void few(const PtArgs& a, char* lds, int block) {
   const int q_hi = (int)min((int64_t)s.keys, max(s.pos0 + 1, (int64_t)0));
   const int64_t q_lo = a.window ? s.pos0 + s.n - a.window : 0;
 
-  // the keys or the values of tile t0 to LDS; pages found one a lane
+  // Where the wave's tiles lie: pages are looked up for 16 tiles at once, one
+  // group of 8 tokens (which lie in one page) a lane, lane 4 (tile mod 16) +
+  // group.  A lookup per tile would be waited for with all loads behind it.
   constexpr int RL = 64 / C::CH;                       // rows of one load
   const int lrow = lane / C::CH, lch = lane % C::CH;
   const char* const kbase = a.pool.k + sizeof(T) * head * a.pool.ks[2];
   const char* const vbase = a.pool.v + sizeof(T) * head * a.pool.vs[2];
-  auto fetch = [&](bool key, int t0, int page, const char* at) __attribute__((always_inline)) {
+  uint64_t k_at = 0, v_at = 0, there = 0;              // offsets; lanes whose page is there
+  auto look_up = [&](int i) __attribute__((always_inline)) {
+    const int t = begin + (i + (lane >> 2)) * PT_FEW_UNIT + 8 * (lane & 3);
+    const int page = t < end ? checked(a.pool, entry_of(a.pool, b, t)) : -1;
+    k_at = token_offset(a.pool, a.pool.ks, page, t);
+    v_at = token_offset(a.pool, a.pool.vs, page, t);
+    there = __ballot(page >= 0);
+  };
+  // rows of tile i that are not there: by groups, and behind the last key
+  auto gone = [&](int i, int t0) {
+    const uint32_t groups = (uint32_t)(there >> (4 * (i & 15))) & 15u;
+    const uint32_t held = (groups * 0x00204081u & 0x01010101u) * 0xffu;
+    const int left = end - t0;
+    return ~held | (left >= 32 ? 0u : left <= 0 ? ~0u : ~0u << left);
+  };
+  // the keys or the values of tile i to LDS
+  auto fetch = [&](bool key, int i, const char* to) __attribute__((always_inline)) {
     const int64_t (&st)[3] = key ? a.pool.ks : a.pool.vs;
-    const uint64_t offset = token_offset(a.pool, st, page, t0 + (lane & 31));
-    const uint32_t to = lds_offset(at);
 #pragma unroll
     for (int u = 0; u < C::FEW_PER; ++u) {
-      const int row = u * RL;
+      const int row = u * RL, in = row % 8;
       const int ch = key ? key_chunk<HD>(row + lrow, lch) : value_chunk<HD>(row + lrow, lch);
-      load_to_lds(rows_at(key ? kbase : vbase, offset, row),
-                  2 * (lrow * (uint32_t)st[1] + 8 * ch), to + 1024 * u);
+      load_to_lds(rows_at(key ? kbase : vbase, key ? k_at : v_at, 4 * (i & 15) + row / 8),
+                  2 * ((in + lrow) * (uint32_t)st[1] + 8 * ch), lds_offset(to) + 1024 * u);
     }
   };
-  const int mine = lane & 31;
-  auto page_at = [&](int t0, int entry) { return t0 + mine < end ? checked(a.pool, entry) : -1; };
   int odd_from = INT32_MAX, odd_to = -1;               // tiles with infinities or NaN
   // Keys and values have one tile's place each: while weights are computed
   // the values are on their way, and while these are added the next keys.
-  int page = page_at(begin, entry_of(a.pool, b, begin + mine));
-  int next = page_at(begin + PT_FEW_UNIT, entry_of(a.pool, b, begin + PT_FEW_UNIT + mine));
+  uint32_t absent = 0;
   if (begin < end) {
-    fetch(true, begin, page, kt);
-    fetch(false, begin, page, vt);
+    look_up(0);
+    absent = gone(0, begin);
+    fetch(true, 0, kt);
+    fetch(false, 0, vt);
   }
+  int i = 0;
   for (int t0 = begin; t0 < end; t0 += PT_FEW_UNIT) {
-    const uint64_t absent = __ballot(page < 0) & 0xffffffffull;
     wait_loads<C::FEW_PER>();                          // the keys are there
-    const int after = entry_of(a.pool, b, t0 + 2 * PT_FEW_UNIT + mine);
     f16v sc[1];
     typename Vec<T>::v8 p[1][2];
     c.template scores<1>(kt, sc);
     c.template settle<1>(a, t0, absent, sc);
     c.template weights<1>(a, sc, p);
     wait_lds();                                        // the keys have been read
-    fetch(true, t0 + PT_FEW_UNIT, next, kt);
-    wait_loads<C::FEW_PER>();                          // the values (and `after`) are there
+    if ((++i & 15) == 0) look_up(i);
+    fetch(true, i, kt);
+    wait_loads<C::FEW_PER>();                          // the values are there
     if (absent || t0 + 32 > q_hi || t0 < q_lo) {
       bool odd = false;
       int me = lane;
@@ -695,9 +710,8 @@ __device__ __forceinline__ void few(const PtArgs& a, char* lds, int block) {
     }
     c.template add_values<1>(vt, p);
     wait_lds();                                        // the values have been read
-    fetch(false, t0 + PT_FEW_UNIT, next, vt);
-    page = next;
-    next = page_at(t0 + 2 * PT_FEW_UNIT, after);
+    fetch(false, i, vt);
+    absent = gone(i, t0 + PT_FEW_UNIT);
   }
   wait_loads<0>();                                     // no load writes to LDS from here on
   c.see_infinities(a, b, head, odd_from, odd_to, PT_FEW_UNIT, 32);
@@ -770,9 +784,10 @@ __global__ void __launch_bounds__(PT_THREADS, HD == 256 ? 1 : HD == 128 ? 2 : 3)
   else few<T, HD>(a, lds, block);
 }
 
-// Joins the pieces of a row whose keys were cut; a wave.  Its records' first
-// loads (N sums) start on construction, before it is known how many there are:
-// what lies past the row's last piece is anything, and not used.
+// Joins the pieces of a row whose keys were cut: by one wave, or (`shared`) by
+// four that take a quarter of the records each.  The first loads (N sums)
+// start on construction, before it is known how many pieces there are: what
+// lies past the row's last one is anything, and not used.
 template <typename T, int HD, int N> struct Pieces {
   static constexpr int E = HD / 64;
   typedef float vec __attribute__((ext_vector_type(E)));
@@ -780,18 +795,26 @@ template <typename T, int HD, int N> struct Pieces {
   const float* sums;
   float2 ml;
   vec first[N];
+  int from, most;                 // the wave's first record, and how many it has at most
 
   __device__ __forceinline__ Pieces(const PtArgs& a, int64_t rec, int ns) {
     const int lane = threadIdx.x & 63;
-    mls = (const float2*)a.part_ml + rec;
-    sums = a.part + rec * HD + lane * E;
-    ml = mls[lane < ns ? lane : 0];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int quarter = (ns + 3) / 4;
+    from = a.merge_shared ? min(wave * quarter, ns) : 0;
+    most = a.merge_shared ? min(quarter, ns - from) : ns;
+    const int64_t at = rec + min(from, ns - 1);
+    mls = (const float2*)a.part_ml + at;
+    sums = a.part + at * HD + lane * E;
+    ml = mls[lane < most ? lane : 0];
 #pragma unroll
-    for (int x = 0; x < N; ++x) first[x] = *(const vec*)(sums + (x < ns ? x : 0) * HD);
+    for (int x = 0; x < N; ++x) first[x] = *(const vec*)(sums + (x < most ? x : 0) * HD);
   }
 
-  __device__ __forceinline__ void join(const PtArgs& a, int parts, int64_t orow) {
+  __device__ __forceinline__ void join(const PtArgs& a, int all, int64_t orow) {
     const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int parts = max(0, min(all - from, most));
     // 64 pieces at a time, one a lane; then their sums
     float top = -INFINITY, l = 0.f;
     vec o = {};
@@ -823,6 +846,27 @@ template <typename T, int HD, int N> struct Pieces {
       for (int x = i0 ? 0 : N; x < count; ++x)
         o += factor(x) * *(const vec*)(sums + (int64_t)(i0 + x) * HD);
     }
+    if (a.merge_shared) {
+      __shared__ float2 wave_ml[4];
+      __shared__ vec wave_o[4][64];
+      if (lane == 0) wave_ml[wave] = make_float2(top, l);
+      wave_o[wave][lane] = o;
+      __syncthreads();
+      if (wave) return;
+      const float own = top;
+#pragma unroll
+      for (int x = 1; x < 4; ++x) top = fmaxf(top, wave_ml[x].x);
+      const float f0 = own == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(own - top);
+      l *= f0;
+      o *= f0;
+#pragma unroll
+      for (int x = 1; x < 4; ++x) {
+        const float m = wave_ml[x].x;
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        l += f * wave_ml[x].y;
+        o += f * wave_o[x][lane];
+      }
+    }
     const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
     for (int e = 0; e < E; ++e) ((T*)a.out)[orow * HD + lane * E + e] = (T)(o[e] * inv);
@@ -835,16 +879,16 @@ __device__ __forceinline__ int few_parts(const PtArgs& a, const Seq& s) {
   return span_of(a, s, 0, PT_FEW, PT_FEW_UNIT, a.ns_few).parts;
 }
 
-// One wave per row and head (and, where the records of the `few` kind are laid
-// out by sequence, one per such record).  A row's records are found without
-// its sequence, so their first loads are on their way while the sequence is
-// looked up (three round trips to memory one after the other before: 4.4 ->
-// 2.7 us for one token's rows).
+// One wave (shared: one workgroup) per row and head (and, where the records of
+// the `few` kind are laid out by sequence, one per such record).  A row's
+// records are found without its sequence, so their first loads are on their
+// way while the sequence is looked up (three round trips to memory one after
+// the other before: 4.4 -> 2.7 us for one token's rows).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x < a.merge_few) {
-    const int i = blockIdx.x * 4 + wave;               // [B][Hkv][32]
+    const int i = a.merge_shared ? blockIdx.x : blockIdx.x * 4 + wave;   // [B][Hkv][32]
     Pieces<T, HD, 8> p(a, (int64_t)i * a.ns_few, a.ns_few);
     const int r = i % PT_FEW, head = i / PT_FEW % a.pool.Hkv, b = i / PT_FEW / a.pool.Hkv;
     const Seq s = sequence(a, b);
@@ -854,7 +898,8 @@ __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
     p.join(a, parts, (int64_t)(s.first + tok) * a.Hq + head * a.GQ + r - tok * a.GQ);
     return;
   }
-  const int64_t orow = ((int64_t)blockIdx.x - a.merge_few) * 4 + wave;
+  const int64_t block = (int64_t)blockIdx.x - a.merge_few;
+  const int64_t orow = a.merge_shared ? block : block * 4 + wave;
   if (orow >= (int64_t)a.T * a.Hq) return;
   const int row = (int)(orow / a.Hq), head = (int)(orow - (int64_t)row * a.Hq);
   auto look_up = [&](Seq& s) {
@@ -894,7 +939,7 @@ struct PtPlan {
   PagePool pool;
   int64_t slots, many0;
   int ns_few, ns_many, few_blocks, many_blocks, merge_few, merge_rows;
-  bool few_by_row;
+  bool few_by_row, merge_shared;
   size_t off_ml, bytes;
 };
 
@@ -907,15 +952,19 @@ gsrq_status pt_plan(const gsrq_paged_attn* s, const gsrq_pages* pages, PtPlan& p
   const int64_t GQ = s->Hq / pages->Hkv;
   if (s->T * GQ > INT32_MAX / 2 || pages->B > (1 << 20)) return GSRQ_E_UNSUPPORTED;
   const int64_t Hkv = pages->Hkv, B = pages->B, cap = (int64_t)pages->per * pages->page_size;
-  // `few`: pieces for four rounds of two workgroups per CU (lengths differ),
-  // of one round of the four waves at the least
-  // (four at the least where the sequences alone would fill it: one of them may
-  // be much longer than the others); none where the table holds 256 tokens at
-  // most: 8 us a call against 10 with the joining launch; at 700 tokens 16
+  // `few`: pieces that give every CU two workgroups, and where they stay longer
+  // than 512 keys twice as many (lengths differ); of one round of the four waves
+  // at the least.  More, shorter ones cost their starts: 8 sequences of 2048
+  // tokens took 25 us in 1024 workgroups, 19 in 512.  Four pieces at the
+  // least where the sequences alone would fill the GPU: one of them may be much
+  // longer than the others.  None where the table holds 256 tokens at most: 8 us
+  // a call against 10 with the joining launch; at 700 tokens 16 against 11.
   int64_t few = 1;
-  if (cap > 256)
-    few = std::min(std::max<int64_t>(4, (1024 + B * Hkv - 1) / (B * Hkv)),
-                   (cap + PT_FEW_UNIT - 1) / PT_FEW_UNIT);
+  if (cap > 256) {
+    const int64_t once = (512 + B * Hkv - 1) / (B * Hkv);
+    few = std::min(2 * once, std::max(once, cap / 512));
+    few = std::min(std::max<int64_t>(4, few), (cap + PT_FEW_UNIT - 1) / PT_FEW_UNIT);
+  }
   // `many`: none where no sequence can have more than 32 queries; cut until
   // the launch's tiles (not counting the slots that hold none) give every CU two
   // workgroups, into pieces of 256 keys at the least, and no more than 1024
@@ -931,9 +980,13 @@ gsrq_status pt_plan(const gsrq_paged_attn* s, const gsrq_pages* pages, PtPlan& p
   const int64_t few_blocks = B * Hkv * few, many_blocks = p.slots * Hkv * many;
   p.few_by_row = s->T * GQ <= PT_FEW * B;
   const int64_t few_rows = p.few_by_row ? s->T * s->Hq : B * Hkv * PT_FEW;
-  const int64_t merge_few = few > 1 && !p.few_by_row ? few_rows / 4 : 0;
+  // four waves join a row of more than 32 pieces (128 pieces: 137 us a call of
+  // one token over 131072 with one wave, 113 with four)
+  p.merge_shared = std::max(few, many) > 32;
+  const int64_t waves = p.merge_shared ? 4 : 1;
+  const int64_t merge_few = few > 1 && !p.few_by_row ? few_rows * waves / 4 : 0;
   const bool by_row = (few > 1 && p.few_by_row) || (p.slots && many > 1);
-  const int64_t merge_rows = by_row ? (s->T * s->Hq + 3) / 4 : 0;
+  const int64_t merge_rows = by_row ? (s->T * s->Hq * waves + 3) / 4 : 0;
   if (few_blocks + many_blocks > MAX_BLOCKS || merge_few + merge_rows > MAX_BLOCKS)
     return GSRQ_E_UNSUPPORTED;
   p.ns_few = (int)few;
@@ -1004,6 +1057,7 @@ gsrq_status gsrq_attn_paged(const gsrq_paged_attn* s, const gsrq_pages* pages,
   // the sequences bring few rows on average
   a.many_first = !p.few_by_row;
   a.few_by_row = p.few_by_row;
+  a.merge_shared = p.merge_shared;
   a.first_blocks = a.many_first ? p.many_blocks : p.few_blocks;
   a.merge_few = p.merge_few;
   a.many0 = p.many0;

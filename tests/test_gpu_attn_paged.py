@@ -171,6 +171,13 @@ def test_long_context_one_token():
     _check(c)
 
 
+@pytest.mark.parametrize("counts,lens,Hq,Hkv,hd", [([1], [9000], 4, 1, 128), ([40], [20000], 2, 1, 64), ([2, 0, 30], [6000, 5, 7000], 3, 1, 256),
+                                                   ([1, 90], [5000, 4500], 2, 1, 128)])
+def test_many_pieces(counts, lens, Hq, Hkv, hd):
+    """So few heads that the keys are cut into more than 32 pieces, for rows of both kinds."""
+    _check(_case(counts, lens, Hq, Hkv, hd, 16))
+
+
 def test_repeatable():
     c = _dev(_case([1, 60, 1], [3000, 2000, 900], 8, 2, 128, 16))
     first = B.attn_paged(*c, lse=True)
