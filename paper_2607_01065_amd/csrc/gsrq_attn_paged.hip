@@ -83,7 +83,7 @@ struct PtArgs {
   float *part, *part_ml;
   int64_t many0;                  // first record of the `many` kind
   int T, Hq, GQ, ns_few, ns_many, window, slots, first_blocks, merge_few;
-  bool many_first, few_by_row, merge_shared;
+  bool many_first, few_by_row, shared_few, shared_rows;
   float c;                        // scale * log2(e)
 };
 
@@ -185,9 +185,9 @@ template <int HD> struct PtCfg {
   static constexpr int PER = TN * CH / PT_THREADS;     // chunks per thread
   static constexpr int FEW_BYTES = 32 * HD * 2;        // a wave's tile of the `few` kind
   static constexpr int FEW_PER = 32 * CH / 64;         // chunks per lane
-  // LDS of a workgroup: two key and two value tiles and which of them held
-  // infinities or NaN, or for `few` a key and a value tile a
-  // wave (where it also joins its waves' sums)
+  // LDS of a workgroup: two key and two value tiles, and which tiles held
+  // infinities or NaN; for `few` a key and a value tile a wave (where it also
+  // joins its waves' sums)
   static constexpr int FEW_LDS = PT_WAVES * 2 * FEW_BYTES;
   static constexpr int MANY_LDS = 4 * BYTES + 32;
   static constexpr int LDS = FEW_LDS > MANY_LDS ? FEW_LDS : MANY_LDS;
@@ -229,15 +229,20 @@ template <typename T, int HD> struct Columns {
   int see_lo, see_hi;             // keys that the query sees
   int all_lo, all_hi;             // keys that every query of the wave sees
 
-  // Query r of the sequence (rows past the last: a copy of row 0 that sees nothing).
+  // Query r of the sequence.  Rows past the last are copies of row 0 that see
+  // everything, so that they ask for no masks; what they come to is not used.
   __device__ __forceinline__ void start(const PtArgs& a, const Seq& s, int head, int r) {
     const int half = (threadIdx.x >> 5) & 1;
     const bool real = r < s.n * a.GQ;
     const int tok = real ? (uint32_t)r / (uint32_t)a.GQ : 0, g = real ? r - tok * a.GQ : 0;
     const int64_t pos = s.pos0 + tok;
-    see_hi = real ? (int)(pos + 1 < s.keys ? (pos + 1 > 0 ? pos + 1 : 0) : s.keys) : 0;
     const int64_t from = a.window ? pos - a.window + 1 : 0;
-    see_lo = from > 0 ? (int)(from < s.keys ? from : s.keys) : 0;
+    see_hi = pos + 1 < s.keys ? (pos + 1 > 0 ? (int)(pos + 1) : 0) : s.keys;
+    see_lo = from > 0 ? (from < s.keys ? (int)from : s.keys) : 0;
+    if (!real) {
+      see_hi = INT32_MAX;
+      see_lo = 0;
+    }
     const T* qp = (const T*)a.q + (int64_t)(s.first + tok) * a.qst[0] +
                   (int64_t)(head * a.GQ + g) * a.qst[1] + 8 * half;
 #pragma unroll
@@ -472,9 +477,9 @@ __device__ __forceinline__ void many(const PtArgs& a, char* lds, int block) {
   const int begin = w.lo + part * w.step;
   const int end = min(w.hi, begin + w.step);
   // keys that every query of the workgroup sees
-  const int64_t first = s.pos0 + r0 / a.GQ, last = s.pos0 + (r0 + PT_ROWS - 1) / a.GQ;
-  const bool whole = r0 + PT_ROWS <= s.n * a.GQ;
-  const int wg_hi = whole ? (int)min((int64_t)s.keys, first + 1) : 0;
+  const int64_t first = s.pos0 + r0 / a.GQ;
+  const int64_t last = s.pos0 + (min(r0 + PT_ROWS, s.n * a.GQ) - 1) / a.GQ;
+  const int64_t wg_hi = min((int64_t)s.keys, first + 1);
   const int64_t wg_lo = a.window ? last - a.window + 1 : 0;
 
   const int r = r0 + 32 * wave + (lane & 31);
@@ -635,7 +640,7 @@ __device__ __forceinline__ void few(const PtArgs& a, char* lds, int block) {
   Columns<T, HD> c;
   c.start(a, s, head, lane & 31);
   // keys that every query of the sequence sees
-  const int q_hi = (int)min((int64_t)s.keys, max(s.pos0 + 1, (int64_t)0));
+  const int64_t q_hi = min((int64_t)s.keys, s.pos0 + 1);
   const int64_t q_lo = a.window ? s.pos0 + s.n - a.window : 0;
 
   // Where the wave's tiles lie: pages are looked up for 16 tiles at once, one
@@ -796,13 +801,15 @@ template <typename T, int HD, int N> struct Pieces {
   float2 ml;
   vec first[N];
   int from, most;                 // the wave's first record, and how many it has at most
+  bool shared;
 
-  __device__ __forceinline__ Pieces(const PtArgs& a, int64_t rec, int ns) {
+  __device__ __forceinline__ Pieces(const PtArgs& a, int64_t rec, int ns, bool four)
+      : shared(four) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int quarter = (ns + 3) / 4;
-    from = a.merge_shared ? min(wave * quarter, ns) : 0;
-    most = a.merge_shared ? min(quarter, ns - from) : ns;
+    from = shared ? min(wave * quarter, ns) : 0;
+    most = shared ? min(quarter, ns - from) : ns;
     const int64_t at = rec + min(from, ns - 1);
     mls = (const float2*)a.part_ml + at;
     sums = a.part + at * HD + lane * E;
@@ -846,7 +853,7 @@ template <typename T, int HD, int N> struct Pieces {
       for (int x = i0 ? 0 : N; x < count; ++x)
         o += factor(x) * *(const vec*)(sums + (int64_t)(i0 + x) * HD);
     }
-    if (a.merge_shared) {
+    if (shared) {
       __shared__ float2 wave_ml[4];
       __shared__ vec wave_o[4][64];
       if (lane == 0) wave_ml[wave] = make_float2(top, l);
@@ -888,8 +895,8 @@ template <typename T, int HD>
 __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if ((int)blockIdx.x < a.merge_few) {
-    const int i = a.merge_shared ? blockIdx.x : blockIdx.x * 4 + wave;   // [B][Hkv][32]
-    Pieces<T, HD, 8> p(a, (int64_t)i * a.ns_few, a.ns_few);
+    const int i = a.shared_few ? blockIdx.x : blockIdx.x * 4 + wave;     // [B][Hkv][32]
+    Pieces<T, HD, 8> p(a, (int64_t)i * a.ns_few, a.ns_few, a.shared_few);
     const int r = i % PT_FEW, head = i / PT_FEW % a.pool.Hkv, b = i / PT_FEW / a.pool.Hkv;
     const Seq s = sequence(a, b);
     if (!is_few(a, s) || r >= s.n * a.GQ) return;
@@ -899,7 +906,7 @@ __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
     return;
   }
   const int64_t block = (int64_t)blockIdx.x - a.merge_few;
-  const int64_t orow = a.merge_shared ? block : block * 4 + wave;
+  const int64_t orow = a.shared_rows ? block : block * 4 + wave;
   if (orow >= (int64_t)a.T * a.Hq) return;
   const int row = (int)(orow / a.Hq), head = (int)(orow - (int64_t)row * a.Hq);
   auto look_up = [&](Seq& s) {
@@ -913,7 +920,7 @@ __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
   };
   Seq s;
   if (a.few_by_row && a.ns_few > 1) {
-    Pieces<T, HD, 8> p(a, orow * a.ns_few, a.ns_few);
+    Pieces<T, HD, 8> p(a, orow * a.ns_few, a.ns_few, a.shared_rows);
     if (!look_up(s)) return;
     if (is_few(a, s)) {
       const int parts = few_parts(a, s);
@@ -923,11 +930,11 @@ __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
     if (a.ns_many < 2) return;
     const int parts = many_parts(s);
     if (parts < 2) return;
-    Pieces<T, HD, 2> q(a, a.many0 + orow * a.ns_many, a.ns_many);
+    Pieces<T, HD, 2> q(a, a.many0 + orow * a.ns_many, a.ns_many, a.shared_rows);
     q.join(a, parts, orow);
     return;
   }
-  Pieces<T, HD, 2> p(a, a.many0 + orow * a.ns_many, a.ns_many);
+  Pieces<T, HD, 2> p(a, a.many0 + orow * a.ns_many, a.ns_many, a.shared_rows);
   if (!look_up(s) || is_few(a, s)) return;
   const int parts = many_parts(s);
   if (parts > 1) p.join(a, parts, orow);
@@ -939,7 +946,7 @@ struct PtPlan {
   PagePool pool;
   int64_t slots, many0;
   int ns_few, ns_many, few_blocks, many_blocks, merge_few, merge_rows;
-  bool few_by_row, merge_shared;
+  bool few_by_row, shared_few, shared_rows;
   size_t off_ml, bytes;
 };
 
@@ -982,11 +989,11 @@ gsrq_status pt_plan(const gsrq_paged_attn* s, const gsrq_pages* pages, PtPlan& p
   const int64_t few_rows = p.few_by_row ? s->T * s->Hq : B * Hkv * PT_FEW;
   // four waves join a row of more than 32 pieces (128 pieces: 137 us a call of
   // one token over 131072 with one wave, 113 with four)
-  p.merge_shared = std::max(few, many) > 32;
-  const int64_t waves = p.merge_shared ? 4 : 1;
-  const int64_t merge_few = few > 1 && !p.few_by_row ? few_rows * waves / 4 : 0;
+  p.shared_few = few > 32;
+  p.shared_rows = many > 32 || (p.few_by_row && few > 32);
+  const int64_t merge_few = few > 1 && !p.few_by_row ? few_rows / (p.shared_few ? 1 : 4) : 0;
   const bool by_row = (few > 1 && p.few_by_row) || (p.slots && many > 1);
-  const int64_t merge_rows = by_row ? (s->T * s->Hq * waves + 3) / 4 : 0;
+  const int64_t merge_rows = !by_row ? 0 : p.shared_rows ? s->T * s->Hq : (s->T * s->Hq + 3) / 4;
   if (few_blocks + many_blocks > MAX_BLOCKS || merge_few + merge_rows > MAX_BLOCKS)
     return GSRQ_E_UNSUPPORTED;
   p.ns_few = (int)few;
@@ -1057,7 +1064,8 @@ gsrq_status gsrq_attn_paged(const gsrq_paged_attn* s, const gsrq_pages* pages,
   // the sequences bring few rows on average
   a.many_first = !p.few_by_row;
   a.few_by_row = p.few_by_row;
-  a.merge_shared = p.merge_shared;
+  a.shared_few = p.shared_few;
+  a.shared_rows = p.shared_rows;
   a.first_blocks = a.many_first ? p.many_blocks : p.few_blocks;
   a.merge_few = p.merge_few;
   a.many0 = p.many0;
