@@ -1,6 +1,7 @@
 // Private header shared by the translation units of libgsrq (subvectors of
 // d <= 8 in gsrq.hip, wider subvectors in gsrq_wide.hip, per-token weights in
-// gsrq_weights.hip): operand types, the
+// gsrq_weights.hip, decode attention in gsrq_attn.hip, the paged cache in
+// gsrq_paged.hip and gsrq_attn_paged.hip): operand types, the
 // scaling constants of the MFMA distance contraction, small device helpers
 // and host-side launch plumbing.  Everything here has internal linkage except
 // the launch-timing state, which every translation unit shares.
