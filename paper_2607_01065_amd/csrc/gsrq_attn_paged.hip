@@ -524,8 +524,10 @@ __device__ __forceinline__ void many(const PtArgs& a, char* lds, int block) {
   fetch(true, begin, page, kt);
   wait_loads<0>();
   __syncthreads();                                     // (odd_tiles, too)
-  fetch(false, begin, page, vt);
-  fetch(true, begin + C::TN, next, kt + C::BYTES);
+  if (begin < end) {                                   // (none that nothing waits for)
+    fetch(false, begin, page, vt);
+    fetch(true, begin + C::TN, next, kt + C::BYTES);
+  }
   int entry = entry_of(a.pool, b, begin + 2 * C::TN + mine);
   f16v even_scores[NB], odd_scores[NB];
   c.template scores<NB>(kt, even_scores);

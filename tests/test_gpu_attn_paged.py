@@ -104,6 +104,15 @@ def test_rows_that_see_nothing():
     assert torch.all(got[6:] == 0) and torch.all(lse[6:] == -float("inf"))
 
 
+@pytest.mark.parametrize("hd", [64, 128, 256])
+def test_prompts_that_see_nothing(hd):
+    """More rows than one workgroup's queries, all or some of them before the first token, and lengths of zero."""
+    c = _case([200, 150, 90], [40, 0, 130], 4, 2, hd, 16)
+    got, lse = _check(c)
+    assert torch.all(got[:160] == 0) and torch.all(lse[:160] == -float("inf"))
+    assert torch.all(got[200:350] == 0) and torch.all(lse[200:350] == -float("inf"))
+
+
 def test_absent_pages_and_stale_places():
     """Holes in the table, and NaN and infinities in every place that no row sees: pages of nobody, places behind
     a sequence's end in its last page."""
