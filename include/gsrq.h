@@ -491,8 +491,8 @@ gsrq_status gsrq_attn_paged_workspace_bytes(const gsrq_paged_attn* s, const gsrq
  * j > p - window (window > 0) and a page that is there:
  *   out = sum_j e^(scale q.k_j) v_j / sum_j e^(scale q.k_j)
  *   lse = ln sum_j e^(scale q.k_j).
- * A row that sees nothing gets zeros and lse -inf; rows of no sequence are
- * left as they are.  What lies in tokens that a row does not see (stale
+ * A row that sees nothing gets zeros and lse -inf (lengths below zero count
+ * as zero); rows of no sequence are left as they are.  What lies in tokens that a row does not see (stale
  * pages, infinities, NaN) does not reach it.
  *
  *  q                 [T][Hq][head_dim] rows of the pages' type, turned.

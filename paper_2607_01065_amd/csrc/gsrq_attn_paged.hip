@@ -97,9 +97,9 @@ struct Seq {
 __device__ __forceinline__ Seq sequence(const PtArgs& a, int b) {
   Seq s;
   new_rows(a.q_start, b, a.T, s.first, s.n);
-  const int len = a.seq_len[b];
+  const int len = max(a.seq_len[b], 0);
   const int64_t cap = (int64_t)a.pool.per << a.pool.shift;
-  s.keys = len < 0 ? 0 : (len < cap ? len : (int)cap);
+  s.keys = len < cap ? len : (int)cap;
   s.pos0 = (int64_t)len - s.n;
   return s;
 }

@@ -113,6 +113,17 @@ def test_prompts_that_see_nothing(hd):
     assert torch.all(got[200:350] == 0) and torch.all(lse[200:350] == -float("inf"))
 
 
+def test_lengths_below_zero():
+    """They count as zero, down to the type's lowest, for few rows and for many."""
+    c = _case([2, 3, 70, 80, 40], [9, 9, 9, 9, 64], 4, 2, 64, 16)
+    ref = _dev(c)
+    c["lens"][:4] = torch.tensor([-(2 ** 31), -1, -(2 ** 31), -5], dtype=torch.int32)
+    got, lse = B.attn_paged(*_dev(c), lse=True)
+    assert torch.all(got[:155] == 0) and torch.all(lse[:155] == -float("inf"))
+    want, z = B.attn_paged(*ref, lse=True)
+    assert torch.equal(got[155:], want[155:]) and torch.equal(lse[155:], z[155:])
+
+
 def test_absent_pages_and_stale_places():
     """Holes in the table, and NaN and infinities in every place that no row sees: pages of nobody, places behind
     a sequence's end in its last page."""
