@@ -519,7 +519,8 @@ gsrq_status gsrq_attn_paged(const gsrq_paged_attn* s, const gsrq_pages* pages,
  *
  *  kv                code shape: D = Hkv * head_dim, d >= 8, any K, M that
  *                    gsrq_decode takes.
- *  cap               code rows per sequence; seq_len is held inside [0, cap].
+ *  cap               code rows per sequence, at most 2^30; seq_len is held
+ *                    inside [0, cap].
  *  k_codes, v_codes  [B][cap][gsrq_code_words(kv)] uint32 (kv->N >= B * cap).
  *  seq_len           [B] int32.
  *  k_gain, k_shape   codebooks [M][G][K], [M][G][K][d], shapes 16-byte aligned.

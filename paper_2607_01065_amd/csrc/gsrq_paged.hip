@@ -692,6 +692,7 @@ gsrq_status gsrq_paged_restore(const gsrq_pages* pages, const gsrq_shape* kv, in
   if (kv->D != (int64_t)pages->Hkv * pages->head_dim) return GSRQ_E_ARG;
   if (kv->N < (int64_t)pages->B * cap) return GSRQ_E_ARG;
   if (kv->d < 8 || kv->d > 256 || !is_pow2(kv->d)) return GSRQ_E_UNSUPPORTED;
+  if (cap > 1 << 30) return GSRQ_E_UNSUPPORTED;       // (no table holds more)
   if (!k_codes || !v_codes || !seq_len || !k_gain || !k_shape || !v_gain || !v_shape)
     return GSRQ_E_ARG;
   if ((uintptr_t)k_shape % 16 || (uintptr_t)v_shape % 16 || (uintptr_t)theta % 8)

@@ -66,7 +66,8 @@ def test_restore_refuses_pages(kw, status):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(cap=0), 1), (dict(N=199), 1), (dict(D=512), 1), (dict(d=0), 1), (dict(d=4), 2), (dict(d=512), 2), (dict(K=200), 1),
-    (dict(M=0), 1), (dict(codes=None), 1), (dict(shape=PTR + 4), 1), (dict(seq_len=None), 1), (dict(K=1 << 17), 1)])
+    (dict(M=0), 1), (dict(codes=None), 1), (dict(shape=PTR + 4), 1), (dict(seq_len=None), 1), (dict(K=1 << 17), 1),
+    (dict(cap=2 ** 31 - 1, N=2 ** 40), 2)])
 def test_restore_refuses_arguments(kw, status):
     assert _restore(**kw) == status
 
