@@ -209,7 +209,7 @@ struct Slice {
   const uint32_t* codes;
   const float *gain, *shape;
   char* base;
-  int64_t st0, st1;               // page, token (bytes)
+  uint32_t st0, st1;              // page, token (elements)
   bool turn;
   int lo, hi;                     // first elements of the halves in a row of D
   int first;                      // of the lower half in the head
@@ -228,8 +228,8 @@ __device__ __forceinline__ Slice slice_of(const RestoreArgs& a, int sub) {
   s.shape = key ? a.k_shape : a.v_shape;
   s.first = HALF * slice;
   s.base = (key ? a.pool.k : a.pool.v) + (head * st[2] + s.first) * (int64_t)sizeof(TP);
-  s.st0 = st[0] * (int64_t)sizeof(TP);
-  s.st1 = st[1] * (int64_t)sizeof(TP);
+  s.st0 = (uint32_t)st[0];
+  s.st1 = (uint32_t)st[1];
   s.turn = key && a.theta;
   s.lo = head * a.hd + s.first;
   s.hi = s.lo + a.hd / 2;
@@ -247,10 +247,12 @@ __device__ __forceinline__ f4 codeword4(const RestoreArgs& a, const Slice& s, in
   return (f4){gk * v[0], gk * v[1], gk * v[2], gk * v[3]};
 }
 
-// Where a token's slice goes; null: its page is not there.
+// Where a token's slice goes; null: its page is not there.  (Strides fit 32
+// bits in elements: one multiply-add each, where 64-bit products take three.)
 __device__ __forceinline__ char* token_at(const RestoreArgs& a, const Slice& s, int page, int t) {
-  return page < 0 ? nullptr
-                  : s.base + page * s.st0 + (t & ((1 << a.pool.shift) - 1)) * s.st1;
+  const uint32_t in = t & ((1 << a.pool.shift) - 1);
+  const uint64_t at = (uint64_t)(uint32_t)page * s.st0 + (uint64_t)in * s.st1;
+  return page < 0 ? nullptr : s.base + 2 * at;
 }
 
 // All stages' codewords of the slice in LDS (M K rows of 64 L bytes), kept while
@@ -307,10 +309,11 @@ __global__ void __launch_bounds__(PR_ROWS* L, M == 1 ? 4 : 2)
       for (int u = 0; u < PR_SLOTS; ++u) {
         const int r = min(PR_ROWS * u + rg, next_len - 1 - next_t0);
         next_entry[u] = entry_of(a.pool, b, next_t0 + r);
+        const uint32_t* row = rows + (uint32_t)r * (uint32_t)a.words;
 #pragma unroll
         for (int m = 0; m < M; ++m) {
-          next_x[u][m] = read_code<decltype(cross)::value>(a, rows + r * a.words, bx[m]);
-          next_y[u][m] = read_code<decltype(cross)::value>(a, rows + r * a.words, by[m]);
+          next_x[u][m] = read_code<decltype(cross)::value>(a, row, bx[m]);
+          next_y[u][m] = read_code<decltype(cross)::value>(a, row, by[m]);
         }
       }
     });
@@ -438,6 +441,7 @@ __global__ void __launch_bounds__(PS_THREADS) paged_row_decode_stages_kernel(Res
   for (int u = 0; u < S; ++u) acc[u] = (f4){0.f, 0.f, 0.f, 0.f};
   int code[S];
   const uint32_t* rows = s.codes + ((int64_t)b * a.cap + t0) * a.words;
+  const uint32_t words = (uint32_t)a.words, last_word = (nrows - 1) * words;
   load(0);
   if (s.turn) {
     for (int i = tid; i < 32 * (S + PS_ROWS); i += PS_THREADS) {
@@ -452,8 +456,8 @@ __global__ void __launch_bounds__(PS_THREADS) paged_row_decode_stages_kernel(Res
     f4* from = tab[m & 1];
     if (!SHARED || (m & 3) == 0) {
       // (the row opaque: addresses are formed here, not kept across stages)
-      int r = rg;
-      asm volatile("" : "+v"(r));
+      uint32_t first_word = rg * words;
+      asm volatile("" : "+v"(first_word));
       const int mm = SHARED ? min(m + (l & 3), a.M - 1) : m;
       const int64_t bit = ((int64_t)mm * a.G + g) * a.b;
       const CodeBits at = {bit >> 5, (int)(bit & 31)};
@@ -461,10 +465,10 @@ __global__ void __launch_bounds__(PS_THREADS) paged_row_decode_stages_kernel(Res
 #pragma unroll
         for (int u = 0; u < S; ++u)
           code[u] = (int)read_code<decltype(cross)::value>(
-              a, rows + (int64_t)min(u * PS_ROWS + r, nrows - 1) * a.words, at);
+              a, rows + min(first_word + u * PS_ROWS * words, last_word), at);
       });
 #pragma unroll
-      for (int u = 0; u < S; ++u) code[u] = code_of(a, (uint32_t)code[u], at) * 16;
+      for (int u = 0; u < S; ++u) code[u] = code_of(a, (uint32_t)code[u], at) * 256;
     }
     {
 #pragma clang fp contract(off)
@@ -475,14 +479,15 @@ __global__ void __launch_bounds__(PS_THREADS) paged_row_decode_stages_kernel(Res
     // one barrier a stage: who writes stage m + 2 over this buffer has passed
     // stage m + 1's, which all reach only after their gathers of stage m
     __syncthreads();
+    const char* const mine = (const char*)(from + l);
 #pragma unroll
     for (int u = 0; u < S; ++u) {
-      int k = code[u];
+      int k = code[u];                    // in bytes
       if (SHARED) {
         k = __builtin_amdgcn_update_dpp(0, code[u], 0x00, 0xf, 0xf, true);        // the quad's first
         code[u] = __builtin_amdgcn_update_dpp(0, code[u], 0x39, 0xf, 0xf, true);  // and on by one
       }
-      acc[u] += from[k + l];
+      acc[u] += *(const f4*)(mine + k);
     }
   }
   int entry[S];                           // all read at once
@@ -594,11 +599,13 @@ gsrq_status restore_resident(const RestoreArgs& a, hipStream_t st) {
 template <typename TP> gsrq_status restore_launch(const RestoreArgs& a, hipStream_t st) {
   const int64_t B = a.pool.B, nsub = 2ll * a.pool.Hkv * (a.hd / 64);
   const int L = a.hd == 64 ? 4 : 8;
-  if (a.M <= (L == 4 ? 2 : 1) && (int64_t)a.M * a.K * 64 * L <= PR_TABLE) {
+  // (rows of codes so long that a chunk's do not fit 32 bits: from memory)
+  const bool near = a.words <= 1 << 20;
+  if (near && a.M <= (L == 4 ? 2 : 1) && (int64_t)a.M * a.K * 64 * L <= PR_TABLE) {
     if (L == 8) return restore_resident<TP, 1, 8>(a, st);
     return a.M == 1 ? restore_resident<TP, 1, 4>(a, st) : restore_resident<TP, 2, 4>(a, st);
   }
-  if (a.K <= PS_K) {
+  if (near && a.K <= PS_K) {
     // chunks of 640 tokens (fewer fills of the stages' buffers) where they
     // give every CU a workgroup, else of 128
     constexpr int LONG = 10, SHORT = 2;
