@@ -401,15 +401,17 @@ __global__ void __launch_bounds__(PR_ROWS* L, M == 1 ? 4 : 2)
 // Sixteen lanes share a token, four dimensions each (the first eight the lower
 // half), so that a gather touches every bank once, whatever the codes: with
 // eight lanes a token and slices of 32 dimensions the gathers alone took 85 us
-// for 3 x <= 10007 tokens x 1024 of 12 stages.  SHARED (d >= 16): four lanes
-// share a code; each of them holds that of one stage of four, which a DPP
-// broadcast hands out when its turn comes.
+// for 3 x <= 10007 tokens x 1024 of 12 stages.  SHARE lanes have one code (4
+// where d >= 16, all 16 where the slice lies in one subspace): each of them
+// holds that of one stage of SHARE, which a DPP broadcast hands out when its
+// turn comes, so that codes, whose loads are waited for, are read once in
+// SHARE stages (12 stages: 127 us with 4 lanes, 115 with 16).
 constexpr int PS_THREADS = 1024;
 constexpr int PS_ROWS = PS_THREADS / 16;
 constexpr int PS_K = 256;
 constexpr int PS_BUF = PS_K * 16;           // f4 per buffer
 
-template <typename TP, int S, bool SHARED>
+template <typename TP, int S, int SHARE>
 __global__ void __launch_bounds__(PS_THREADS) paged_row_decode_stages_kernel(RestoreArgs a,
                                                                              int nsub) {
   __shared__ __align__(16) f4 tab[2][PS_BUF];
@@ -454,11 +456,11 @@ __global__ void __launch_bounds__(PS_THREADS) paged_row_decode_stages_kernel(Res
   }
   for (int m = 0; m < a.M; ++m) {
     f4* from = tab[m & 1];
-    if (!SHARED || (m & 3) == 0) {
+    if (m % SHARE == 0) {
       // (the row opaque: addresses are formed here, not kept across stages)
       uint32_t first_word = rg * words;
       asm volatile("" : "+v"(first_word));
-      const int mm = SHARED ? min(m + (l & 3), a.M - 1) : m;
+      const int mm = min(m + l % SHARE, a.M - 1);
       const int64_t bit = ((int64_t)mm * a.G + g) * a.b;
       const CodeBits at = {bit >> 5, (int)(bit & 31)};
       by_crossing(a, [&](auto cross) __attribute__((always_inline)) {
@@ -483,9 +485,13 @@ __global__ void __launch_bounds__(PS_THREADS) paged_row_decode_stages_kernel(Res
 #pragma unroll
     for (int u = 0; u < S; ++u) {
       int k = code[u];                    // in bytes
-      if (SHARED) {
-        k = __builtin_amdgcn_update_dpp(0, code[u], 0x00, 0xf, 0xf, true);        // the quad's first
-        code[u] = __builtin_amdgcn_update_dpp(0, code[u], 0x39, 0xf, 0xf, true);  // and on by one
+      // the first of the lanes' codes, and on by one
+      if (SHARE == 4) {
+        k = __builtin_amdgcn_update_dpp(0, code[u], 0x00, 0xf, 0xf, true);
+        code[u] = __builtin_amdgcn_update_dpp(0, code[u], 0x39, 0xf, 0xf, true);
+      } else if (SHARE == 16) {
+        k = __builtin_amdgcn_update_dpp(0, code[u], 0x150, 0xf, 0xf, true);
+        code[u] = __builtin_amdgcn_update_dpp(0, code[u], 0x12f, 0xf, 0xf, true);
       }
       acc[u] += *(const f4*)(mine + k);
     }
@@ -616,12 +622,15 @@ template <typename TP> gsrq_status restore_launch(const RestoreArgs& a, hipStrea
     if (blocks > (1 << 22) - 1) return GSRQ_E_UNSUPPORTED;
     const unsigned n = (unsigned)blocks;
     const int i = (int)nsub;
+    auto launch = [&](auto kern) { kern<<<n, PS_THREADS, 0, st>>>(a, i); };
     if (is_long) {
-      if (a.d >= 16) paged_row_decode_stages_kernel<TP, LONG, true><<<n, PS_THREADS, 0, st>>>(a, i);
-      else paged_row_decode_stages_kernel<TP, LONG, false><<<n, PS_THREADS, 0, st>>>(a, i);
+      if (a.d >= a.hd) launch(paged_row_decode_stages_kernel<TP, LONG, 16>);
+      else if (a.d >= 16) launch(paged_row_decode_stages_kernel<TP, LONG, 4>);
+      else launch(paged_row_decode_stages_kernel<TP, LONG, 1>);
     } else {
-      if (a.d >= 16) paged_row_decode_stages_kernel<TP, SHORT, true><<<n, PS_THREADS, 0, st>>>(a, i);
-      else paged_row_decode_stages_kernel<TP, SHORT, false><<<n, PS_THREADS, 0, st>>>(a, i);
+      if (a.d >= a.hd) launch(paged_row_decode_stages_kernel<TP, SHORT, 16>);
+      else if (a.d >= 16) launch(paged_row_decode_stages_kernel<TP, SHORT, 4>);
+      else launch(paged_row_decode_stages_kernel<TP, SHORT, 1>);
     }
     return launch_ok();
   }
