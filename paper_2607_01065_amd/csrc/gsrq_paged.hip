@@ -535,7 +535,7 @@ __global__ void __launch_bounds__(PS_THREADS) paged_row_decode_stages_kernel(Res
   }
 }
 
-// Codebooks of more than 512 codewords, which LDS does not hold: a lane per 16
+// Codebooks of more codewords than the kernels above hold in LDS: a lane per 16
 // elements of a head of one token's key or value row, codewords from memory.
 template <typename TP>
 __global__ void __launch_bounds__(PA_THREADS) paged_row_decode_kernel(RestoreArgs a) {
