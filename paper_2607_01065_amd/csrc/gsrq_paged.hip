@@ -423,7 +423,9 @@ __global__ void __launch_bounds__(PS_THREADS) paged_row_decode_stages_kernel(Res
   const int b = chunk / per, t0 = (chunk - b * per) * PS_ROWS * S;
   const int len = min(a.seq_len[b], a.cap);
   if (t0 >= len) return;
-  const int nrows = len - t0;
+  // (of this chunk alone: all that are left times their words would not fit
+  // 32 bits in long contexts)
+  const int nrows = min(len - t0, PS_ROWS * S);
   const int e = (l < 8 ? s.lo : s.hi - 32) + 4 * l, g = e / a.d;
   constexpr int PER = PS_BUF / PS_THREADS;
   f4 v[PER];

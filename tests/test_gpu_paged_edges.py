@@ -1,0 +1,62 @@
+"""Ends of the paged cache's documented ranges: contexts whose codes pass 2^32
+words, layouts that run kernels of their own, infinities of small weight,
+values at the pages' type's end."""
+import numpy as np
+import pytest
+
+from tests import paged_ref as R
+from tests.gpu_util import say
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2607_01065_amd import gsrq as B  # noqa: E402
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    B.load_library()
+
+
+def _codeword_sums(codes, gain, shape, dtype):
+    """Rows [tokens, G * d] of codes [tokens, M, G]: codewords rounded to float32, summed in float32 in stage order,
+    rounded once: every bit as paged_restore documents it."""
+    x = torch.zeros((codes.shape[0], shape.shape[1], shape.shape[3]), dtype=torch.float32, device=codes.device)
+    g = torch.arange(shape.shape[1], device=codes.device)
+    for m in range(shape.shape[0]):
+        c = codes[:, m].long()
+        x = x + gain[m][g, c][..., None] * shape[m][g, c]
+    return x.flatten(1).to(dtype)
+
+
+def test_restore_past_32_bit_code_words():
+    """A context of 2^24 + 1000 tokens of 256 code words each, of which a few hundred have pages: the first tokens, where
+    the words that are left just pass 2^32, and the last."""
+    M, G, d, Hkv, hd, page = 64, 16, 8, 1, 128, 16
+    L, words = 2 ** 24 + 1000, M * G // 4
+    if torch.cuda.mem_get_info()[0] < 28 << 30:
+        pytest.skip("less than 28 GiB free")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    gain, shape = torch.rand((M, G, 256), generator=g, device="cuda"), torch.randn((M, G, 256, d), generator=g, device="cuda")
+    codes = torch.zeros((1, L, words), dtype=torch.int32, device="cuda")
+    per = -(-L // page)
+    table = torch.full((1, per), -1, dtype=torch.int32)
+    held = list(range(96)) + list(range(per - 8, per))               # tokens 0 .. 1535 and the last 120
+    table[0, held] = torch.arange(len(held), dtype=torch.int32)
+    at = torch.cat([torch.arange(page * i, page * i + page) for i in held])
+    at = at[at < L].cuda()
+    drawn = torch.randint(0, 256, (at.numel(), M, G), generator=g, device="cuda", dtype=torch.uint8)
+    codes[0, at] = drawn.view(at.numel(), M * G).view(torch.int32)
+    kp, vp = (torch.full((len(held), page, Hkv, hd), 9.0, dtype=torch.float16, device="cuda") for _ in range(2))
+    say("restore", L, "tokens,", words, "words each")
+    B.paged_restore(codes, codes, torch.tensor([L], dtype=torch.int32, device="cuda"), gain, shape, -gain, shape, kp, vp,
+                    table.cuda())
+    torch.cuda.synchronize()
+    want = _codeword_sums(drawn, gain, shape, torch.float16)
+    for pool, ref in ((kp, want), (vp, -want)):
+        rows = pool.view(-1, hd)
+        wrong = (rows[: at.numel()] != ref).any(1)
+        assert not wrong.any(), f"{int(wrong.sum())} tokens, the first {int(at[wrong][0])}"
+        assert torch.all(rows[at.numel():] == 9.0)                   # places behind the end
