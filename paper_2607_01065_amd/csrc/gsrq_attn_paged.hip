@@ -959,7 +959,9 @@ gsrq_status pt_plan(const gsrq_paged_attn* s, const gsrq_pages* pages, PtPlan& p
     return GSRQ_E_ARG;
   if (!(s->scale > 0.f) || !(s->scale < INFINITY)) return GSRQ_E_ARG;
   const int64_t GQ = s->Hq / pages->Hkv;
-  if (s->T * GQ > INT32_MAX / 2 || pages->B > (1 << 20)) return GSRQ_E_UNSUPPORTED;
+  // (T by itself first: its product with GQ is taken in 64 bits)
+  if (s->T > INT32_MAX / 2 || s->T * GQ > INT32_MAX / 2 || pages->B > (1 << 20))
+    return GSRQ_E_UNSUPPORTED;
   const int64_t Hkv = pages->Hkv, B = pages->B, cap = (int64_t)pages->per * pages->page_size;
   // `few`: pieces that give every CU two workgroups, and where they stay longer
   // than 512 keys twice as many (lengths differ); of one round of the four waves
