@@ -792,7 +792,7 @@ def paged_restore(k_codes, v_codes, seq_len, k_gain, k_shape, v_gain, v_shape, k
                           ("v_gain", v_gain, (M, G, K)), ("v_shape", v_shape, (M, G, K, d))):
         _need(t, name, (torch.float32,), dev, size)
     _need(theta, "theta", (torch.float64,), dev, (hd // 2,))
-    if cap == 0:
+    if B == 0 or cap == 0:
         return
 
     def call():

@@ -22,3 +22,13 @@ def test_attention_refuses_rows_whose_queries_pass_any_size(T):
     s = B.PagedAttn(T, 32, 0, 0.1, 0)
     status = B.load_library().gsrq_attn_paged_workspace_bytes(ctypes.byref(s), ctypes.byref(pages), ctypes.byref(n))
     assert (status, n.value) == (B.GSRQ_E_UNSUPPORTED, 7)
+
+
+@pytest.mark.parametrize("B_,cap", [(0, 5), (2, 0), (0, 0)])
+def test_restore_of_nothing_returns(B_, cap):
+    """No sequences or no code rows: nothing runs, as for appending and attention without rows."""
+    kp = torch.zeros((4, 8, 2, 64), dtype=torch.float16)
+    codes = torch.zeros((B_, cap, 4), dtype=torch.int32)
+    gain, shape = torch.zeros((1, 16, 256)), torch.zeros((1, 16, 256, 8))
+    assert B.paged_restore(codes, codes, torch.zeros(B_, dtype=torch.int32), gain, shape, gain, shape, kp, kp,
+                           torch.zeros((B_, 2), dtype=torch.int32)) is None
