@@ -737,7 +737,7 @@ def attn_paged(q, k_pages, v_pages, table, q_start, seq_len, *, scale=None, wind
         raise ValueError(f"workspace must be contiguous, on {k_pages.device}")
     try:
         s = _PAGED_ATTN.pack(T, Hq, window, hd ** -0.5 if scale is None else scale, 0)
-    except struct.error:
+    except (struct.error, ZeroDivisionError):        # (heads of no elements)
         raise ValueError("window must be a number of tokens, or 0, and scale a number") from None
 
     def call():

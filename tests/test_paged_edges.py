@@ -1,6 +1,6 @@
 """Ends of the ranges that the paged cache's entry points check before any GPU
-work, on the CPU: sizes whose products pass 64 bits, empty batches, numbers
-that fit no float32."""
+work, on the CPU: sizes whose products pass 64 bits, empty batches, heads of no
+elements."""
 import ctypes
 import os
 
@@ -32,3 +32,11 @@ def test_restore_of_nothing_returns(B_, cap):
     gain, shape = torch.zeros((1, 16, 256)), torch.zeros((1, 16, 256, 8))
     assert B.paged_restore(codes, codes, torch.zeros(B_, dtype=torch.int32), gain, shape, gain, shape, kp, kp,
                            torch.zeros((B_, 2), dtype=torch.int32)) is None
+
+
+def test_attention_refuses_heads_of_no_elements():
+    """They have no default scale; refused as any other head size is."""
+    kp = torch.zeros((4, 8, 2, 0), dtype=torch.float16)
+    with pytest.raises(ValueError):
+        B.attn_paged(torch.zeros((3, 4, 0), dtype=torch.float16), kp, kp, torch.zeros((2, 2), dtype=torch.int32),
+                     torch.zeros(3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
