@@ -492,8 +492,9 @@ gsrq_status gsrq_attn_paged_workspace_bytes(const gsrq_paged_attn* s, const gsrq
  *   out = sum_j e^(scale q.k_j) v_j / sum_j e^(scale q.k_j)
  *   lse = ln sum_j e^(scale q.k_j).
  * A row that sees nothing gets zeros and lse -inf (lengths below zero count
- * as zero); rows of no sequence are left as they are.  What lies in tokens that a row does not see (stale
- * pages, infinities, NaN) does not reach it.
+ * as zero); rows of no sequence are left as they are.  What lies in tokens that
+ * a row does not see (stale pages, infinities, NaN) does not reach it; an
+ * infinity or NaN among the values that it sees does, however small its weight.
  *
  *  q                 [T][Hq][head_dim] rows of the pages' type, turned.
  *  out               [T][Hq][head_dim] of the pages' type, 16-byte aligned.

@@ -25,7 +25,9 @@
 // weights are 2^(s - m + 6): at most 2^14, and the float16 subnormals, which
 // lose bits, begin 2^-20 below the maximum.  Weights are rounded to the
 // pages' type for the product alone (their own sum, which is also a result,
-// is of the unrounded ones); all sums are float32.
+// is of the unrounded ones); all sums are float32.  A weight that comes to zero
+// makes NaN of an infinite value: such sums are looked through again at the
+// end (a check of the sums, 0.2 to 0.5 us a call).
 #include <algorithm>
 
 #include "gsrq_paged.h"
@@ -218,6 +220,40 @@ __device__ __forceinline__ uint32_t lds_offset(const char* p) {
   return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const lds_char*)p);
 }
 
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY; }
+
+// o + f x for a factor f >= 0 that stands for a weight above zero, however
+// small: an infinity stays one where f has come to zero.
+__device__ __forceinline__ float add_weighted(float o, float f, float x) {
+  return is_finite(x) ? fmaf(f, x, o) : o + x;
+}
+
+// Takes infinities and NaN out of eight values; whether there were any.
+template <typename T> __device__ __forceinline__ bool finite_pairs(u4& x) {
+  constexpr uint32_t HI = Vec<T>::EXP & 0xffff0000u, LO = Vec<T>::EXP & 0xffffu;
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t w = x[i];
+    if ((w & LO) == LO) w &= 0xffff0000u;
+    if ((w & HI) == HI) w &= 0xffffu;
+    any = any || w != x[i];
+    x[i] = w;
+  }
+  return any;
+}
+
+// Takes infinities and NaN out of a 16-byte chunk of values in a tile where
+// some query does not see every row (its weight of zero would make NaN of
+// them); add_infinities() brings them to the queries that see them.  Whether
+// there were any.
+template <typename T> __device__ __forceinline__ bool without_infinities(u4* at) {
+  u4 x = *at;
+  const bool any = finite_pairs<T>(x);
+  if (any) *at = x;
+  return any;
+}
+
 // One wave's queries, as columns: the lane's query, and its part of the sums.
 template <typename T, int HD> struct Columns {
   typedef typename Vec<T>::v8 v8;
@@ -362,21 +398,32 @@ template <typename T, int HD> struct Columns {
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 
-  // After the last tile: the infinities and NaN that without_infinities() took
-  // out, of `rows` keys every `step` from `from` to `to`, for the queries that
-  // see them.  A weight above zero leaves them what they are, and adding one
-  // twice changes nothing.
+  // Adds the infinities and NaN among the values of `rows` keys every `step`
+  // from `from` to `to`, for the queries that see them.  A weight above zero
+  // leaves them what they are, and adding one twice changes nothing.
   __device__ __forceinline__ void see_infinities(const PtArgs& a, int b, int head, int from, int to,
                                                  int step, int rows) {
-    const int half = (threadIdx.x >> 5) & 1;
-    for (int t0 = from; t0 <= to; t0 += step)
-      for (int j = t0; j < t0 + rows; ++j) {
-        const int page = page_of(a.pool, b, j);
-        const bool seen = page >= 0 && j < see_hi && j >= see_lo;
-        if (!__any(seen)) continue;
-        const T* v = (const T*)a.pool.v + page * a.pool.vs[0] +
-                     (int64_t)(j & ((1 << a.pool.shift) - 1)) * a.pool.vs[1] +
-                     head * a.pool.vs[2] + 4 * half;
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    const auto value = [&](int page, int j) __attribute__((always_inline)) {
+      return (const T*)a.pool.v + page * a.pool.vs[0] +
+             (int64_t)(j & ((1 << a.pool.shift) - 1)) * a.pool.vs[1] + head * a.pool.vs[2];
+    };
+    for (int t0 = from; t0 <= to; t0 += step) {
+      // one key a lane: whether it holds any
+      const int mine = lane < rows ? page_of(a.pool, b, t0 + lane) : -1;
+      bool odd = false;
+      if (mine >= 0) {
+        const T* v = value(mine, t0 + lane);
+#pragma unroll 4
+        for (int c = 0; c < HD / 8; ++c) {
+          u4 x = *(const u4*)(v + 8 * c);
+          odd = finite_pairs<T>(x) || odd;
+        }
+      }
+      for (uint64_t todo = __ballot(odd); todo; todo &= todo - 1) {
+        const int j = t0 + __builtin_ctzll(todo);
+        const T* v = value(__builtin_amdgcn_readlane(mine, j - t0), j) + 4 * half;
+        const bool seen = j < see_hi && j >= see_lo;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -385,32 +432,57 @@ template <typename T, int HD> struct Columns {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float y = (float)x[e];
-              o[t][4 * i + e] += seen && !(fabsf(y) < INFINITY) ? y : 0.f;
+              o[t][4 * i + e] += seen && !is_finite(y) ? y : 0.f;
             }
           }
       }
+    }
+  }
+
+  // After the last tile, l joined: the infinities and NaN that the sums lack.
+  // They are those that without_infinities() took out, in the tiles from
+  // `odd_from` to `odd_to`; and where a sum is NaN though no score was (`real`:
+  // the lane's query is one), any of the piece's, whose tiles start at `begin`
+  // and end before `end`: a weight that is zero in the pages' type, or that a
+  // later maximum made zero, has made NaN of an infinity that the query sees.
+  __device__ __forceinline__ void add_infinities(const PtArgs& a, int b, int head, bool real,
+                                                 int odd_from, int odd_to, int begin, int end,
+                                                 int step, int rows) {
+    // (NaN if any of them is; infinities of both signs look the same, and change nothing)
+    f16v sum = o[0];
+#pragma unroll
+    for (int t = 1; t < DT; ++t) sum += o[t];
+#pragma unroll
+    for (int i = 2; i < 16; ++i) sum[i & 1] += sum[i];
+    const float all = sum[0] + sum[1];
+    const bool again = __any(all != all && real && l == l);
+    // (rare: what follows lies apart from the code of every call)
+    if (__builtin_expect(!again && odd_from > odd_to, 1)) return;
+    uint32_t nan[(DT + 1) / 2] = {};
+    if (again) {
+      odd_from = begin;
+      odd_to = end - 1;
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const bool is = o[t][i] != o[t][i];
+          nan[t / 2] |= is ? 1u << (16 * (t & 1) + i) : 0u;
+          o[t][i] = is ? 0.f : o[t][i];
+        }
+    }
+    see_infinities(a, b, head, odd_from, odd_to, step, rows);
+    if (again) {                                       // NaN of another cause stays
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const bool was = (nan[t / 2] >> (16 * (t & 1) + i)) & 1u;
+          o[t][i] = was && is_finite(o[t][i]) ? NAN : o[t][i];
+        }
+    }
   }
 };
-
-// Takes infinities and NaN out of a 16-byte chunk of values in a tile where
-// some query does not see every row (its weight of zero would make NaN of
-// them); see_infinities() brings them to the queries that see them.  Whether
-// there were any.
-template <typename T> __device__ __forceinline__ bool without_infinities(u4* at) {
-  constexpr uint32_t HI = Vec<T>::EXP & 0xffff0000u, LO = Vec<T>::EXP & 0xffffu;
-  u4 x = *at;
-  bool any = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t w = x[i];
-    if ((w & LO) == LO) w &= 0xffff0000u;
-    if ((w & HI) == HI) w &= 0xffffu;
-    any = any || w != x[i];
-    x[i] = w;
-  }
-  if (any) *at = x;
-  return any;
-}
 
 // Where a lane's token lies from its head's first key (or value) on, in bytes;
 // an absent page counts as the pool's first, which nobody looks at.  Taken one
@@ -596,12 +668,12 @@ __device__ __forceinline__ void many(const PtArgs& a, char* lds, int block) {
     step(t0 + C::TN, 1, odd_scores, even_scores);
   }
   __syncthreads();
-  c.see_infinities(a, b, head, __builtin_amdgcn_readfirstlane(odd_tiles[0]),
-                   __builtin_amdgcn_readfirstlane(odd_tiles[1]), C::TN, C::TN);
-
   const float2 ls = both_halves(c.l);
   c.l = ls.x + ls.y;
-  if (r >= s.n * a.GQ) return;
+  const bool real = r < s.n * a.GQ;
+  c.add_infinities(a, b, head, real, __builtin_amdgcn_readfirstlane(odd_tiles[0]),
+                   __builtin_amdgcn_readfirstlane(odd_tiles[1]), begin, end, C::TN, C::TN);
+  if (!real) return;
   const int tok = r / a.GQ, g = r - tok * a.GQ;
   const int64_t orow = (int64_t)(s.first + tok) * a.Hq + head * a.GQ + g;
   if (w.parts == 1) {
@@ -618,6 +690,26 @@ __device__ __forceinline__ void many(const PtArgs& a, char* lds, int block) {
       *(f4*)(dst + 32 * t + 8 * i) =
           (f4){c.o[t][4 * i], c.o[t][4 * i + 1], c.o[t][4 * i + 2], c.o[t][4 * i + 3]};
   if (half == 0) *(float2*)(a.part_ml + 2 * rec) = make_float2(c.m, c.l);
+}
+
+// The same for four of a row's sums, from dimension `dim` on, over a piece
+// of the keys: where one is NaN, what the row sees there that is not finite.
+template <typename T>
+__device__ __forceinline__ void see_row_infinities(const PtArgs& a, const Seq& s, int b, int head,
+                                                   int tok, int dim, int from, int to, f4& o) {
+  const int64_t pos = s.pos0 + tok, low = a.window ? pos - a.window + 1 : 0;
+  f4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int64_t j = low > from ? low : from; j < to && j <= pos; ++j) {
+    const int page = page_of(a.pool, b, j);
+    if (page < 0) continue;
+    const T* v = (const T*)a.pool.v + page * a.pool.vs[0] +
+                 (j & ((1 << a.pool.shift) - 1)) * a.pool.vs[1] + head * a.pool.vs[2] + dim;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] += is_finite((float)v[e]) ? 0.f : (float)v[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = o[e] != o[e] && !is_finite(y[e]) ? y[e] : o[e];
 }
 
 // All queries (32 at most) of one sequence and key head, and a piece of the
@@ -764,6 +856,12 @@ __device__ __forceinline__ void few(const PtArgs& a, char* lds, int block) {
       for (int e = 0; e < 4; ++e) o[e] += f * v[e];
     }
     const int tok = r / a.GQ, g = r - tok * a.GQ;
+    bool lost = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) lost = lost || o[e] != o[e];
+    if (__builtin_expect(lost && l == l, 0))
+      see_row_infinities<T>(a, s, b, head, tok, 4 * ch, w.lo + part * w.step,
+                            min(w.hi, w.lo + (part + 1) * w.step), o);
     const int64_t orow = (int64_t)(s.first + tok) * a.Hq + head * a.GQ + g;
     if (w.parts == 1) {
       const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -798,6 +896,16 @@ __global__ void __launch_bounds__(PT_THREADS, HD == 256 ? 1 : HD == 128 ? 2 : 3)
 template <typename T, int HD, int N> struct Pieces {
   static constexpr int E = HD / 64;
   typedef float vec __attribute__((ext_vector_type(E)));
+  static __device__ __forceinline__ void add_sums(vec& o, float f, vec x) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = add_weighted(o[e], f, x[e]);
+  }
+  static __device__ __forceinline__ bool any_nan(vec o) {
+    bool nan = false;
+#pragma unroll
+    for (int e = 0; e < E; ++e) nan = nan || o[e] != o[e];
+    return __any(nan);
+  }
   const float2* mls;
   const float* sums;
   float2 ml;
@@ -855,6 +963,14 @@ template <typename T, int HD, int N> struct Pieces {
       for (int x = i0 ? 0 : N; x < count; ++x)
         o += factor(x) * *(const vec*)(sums + (int64_t)(i0 + x) * HD);
     }
+    if (__builtin_expect(any_nan(o), 0)) {             // a factor of zero, perhaps: once more
+      o = (vec){};
+      for (int x = 0; x < parts; ++x) {
+        const float m = mls[x].x;
+        add_sums(o, m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top),
+                 *(const vec*)(sums + (int64_t)x * HD));
+      }
+    }
     if (shared) {
       __shared__ float2 wave_ml[4];
       __shared__ vec wave_o[4][64];
@@ -874,6 +990,13 @@ template <typename T, int HD, int N> struct Pieces {
         const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
         l += f * wave_ml[x].y;
         o += f * wave_o[x][lane];
+      }
+      if (__builtin_expect(any_nan(o), 0)) {
+        o = (vec){};
+        for (int x = 0; x < 4; ++x) {
+          const float m = wave_ml[x].x;
+          add_sums(o, m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top), wave_o[x][lane]);
+        }
       }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;

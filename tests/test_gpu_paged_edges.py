@@ -60,3 +60,45 @@ def test_restore_past_32_bit_code_words():
         wrong = (rows[: at.numel()] != ref).any(1)
         assert not wrong.any(), f"{int(wrong.sum())} tokens, the first {int(at[wrong][0])}"
         assert torch.all(rows[at.numel():] == 9.0)                   # places behind the end
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("low", [8.0, 16.0])
+@pytest.mark.parametrize("counts,lens,hd,until", [
+    ([1], [100], 64, 33),                   # one piece; all of one wave's keys
+    ([1, 3], [3000, 900], 128, 300),        # pieces that hold nothing else
+    ([2], [2500], 256, 140),
+    ([200], [500], 128, 140),               # many rows, tiles before all of them
+    ([150, 1], [1500, 40], 64, 70),
+    ([70], [1200], 256, 300),
+])
+def test_infinities_of_small_weight(counts, lens, hd, until, low, dtype):
+    """Infinities and NaN in values that every row sees, at keys whose scores lie far below the others' (75 and 150 in
+    log2 at heads of 64, twice that at 256): weights that are zero in float16, or in float32, are above zero all the
+    same, so an infinity reaches the row, and where it is the first thing seen a later maximum does not undo it."""
+    from tests.test_gpu_attn_paged import _case, _check
+    c = _case(counts, lens, 4, 2, hd, 16, dtype)
+    c["q"] = c["q"].abs()
+    pages, page = c["kp"].shape[:2]
+    bad = [float("inf"), -float("inf"), float("nan")]
+    for b, L in enumerate(lens):
+        n = counts[b]
+        for t in range(min(until, L - n)):
+            c["kp"][R.page_of(c["tab"], pages, page, b, t), t % page] = -low
+        for i, t in enumerate((1, 2, min(until, L - n) - 1)):
+            c["vp"][R.page_of(c["tab"], pages, page, b, t), t % page, :, 5 * i + b] = bad[i]
+    got, lse = _check(c)
+    assert torch.isinf(got).any() and torch.isnan(got).any() and torch.isfinite(lse).all()
+
+
+def test_scores_of_nan_stay_with_their_row():
+    """A row whose query or visible key is NaN gets NaN, whatever the values hold; its neighbours do not."""
+    from tests.test_gpu_attn_paged import ORDER, _case
+    for counts, lens in (([2], [700]), ([90], [300])):
+        c = _case(counts, lens, 4, 2, 128, 16)
+        ref = B.attn_paged(*(c[n].cuda() for n in ORDER))
+        c["q"][1, 2, 7] = float("nan")
+        got, lse = B.attn_paged(*(c[n].cuda() for n in ORDER), lse=True)
+        assert torch.isnan(got[1, 2]).all() and torch.isnan(lse[1, 2])
+        ref[1, 2] = got[1, 2] = 0
+        assert torch.equal(got, ref)
