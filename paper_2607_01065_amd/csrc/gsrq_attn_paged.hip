@@ -54,6 +54,7 @@ template <> struct Vec<_Float16> {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
   static constexpr uint32_t EXP = 0x7c007c00u;         // exponent bits of a pair
+  static constexpr float MAX = 65504.f;
   static __device__ __forceinline__ h4 read_tr(lds_char* p) {
     typedef __fp16 fp16x4 __attribute__((ext_vector_type(4)));
     return __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4f16(
@@ -67,6 +68,7 @@ template <> struct Vec<__bf16> {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
   static constexpr uint32_t EXP = 0x7f807f80u;
+  static constexpr float MAX = 0x1.fep127f;
   static __device__ __forceinline__ b4 read_tr(lds_char* p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) b4*)p);
   }
@@ -226,6 +228,13 @@ __device__ __forceinline__ bool is_finite(float x) { return fabsf(x) < INFINITY;
 // small: an infinity stays one where f has come to zero.
 __device__ __forceinline__ float add_weighted(float o, float f, float x) {
   return is_finite(x) ? fmaf(f, x, o) : o + x;
+}
+
+// An element of a result.  Weights are rounded and their sum is not, so a mean
+// of values at the type's end can come out past it by a rounding (in float16
+// 2^-11 of itself); it is held inside.
+template <typename T> __device__ __forceinline__ T result(float x) {
+  return (T)(is_finite(x) ? __builtin_amdgcn_fmed3f(x, -Vec<T>::MAX, Vec<T>::MAX) : x);
 }
 
 // Takes infinities and NaN out of eight values; whether there were any.
@@ -515,7 +524,7 @@ __device__ __forceinline__ void put_row(const PtArgs& a, const Columns<T, HD>& c
     for (int i = 0; i < 4; ++i) {
       v4 x;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = (T)(c.o[t][4 * i + e] * inv);
+      for (int e = 0; e < 4; ++e) x[e] = result<T>(c.o[t][4 * i + e] * inv);
       *(v4*)(dst + 32 * t + 8 * i) = x;
     }
   if (a.lse && half == 0)
@@ -867,7 +876,7 @@ __device__ __forceinline__ void few(const PtArgs& a, char* lds, int block) {
       const float inv = l == 0.f ? 0.f : 1.f / l;
       typename Vec<T>::v4 x;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = (T)(o[e] * inv);
+      for (int e = 0; e < 4; ++e) x[e] = result<T>(o[e] * inv);
       *(typename Vec<T>::v4*)((T*)a.out + orow * HD + 4 * ch) = x;
       if (a.lse && ch == 0)
         a.lse[orow] = l == 0.f ? -INFINITY : (top - PT_SHIFT + log2f(l)) * 0.69314718055994531f;
@@ -1001,7 +1010,7 @@ template <typename T, int HD, int N> struct Pieces {
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-    for (int e = 0; e < E; ++e) ((T*)a.out)[orow * HD + lane * E + e] = (T)(o[e] * inv);
+    for (int e = 0; e < E; ++e) ((T*)a.out)[orow * HD + lane * E + e] = result<T>(o[e] * inv);
     if (a.lse && lane == 0)
       a.lse[orow] = l == 0.f ? -INFINITY : (top - PT_SHIFT + log2f(l)) * 0.69314718055994531f;
   }

@@ -102,3 +102,25 @@ def test_scores_of_nan_stay_with_their_row():
         assert torch.isnan(got[1, 2]).all() and torch.isnan(lse[1, 2])
         ref[1, 2] = got[1, 2] = 0
         assert torch.equal(got, ref)
+
+
+@pytest.mark.parametrize("counts,lens,hd", [([1], [90], 64), ([3, 1], [2000, 700], 128), ([1], [9000], 256),
+                                            ([200], [400], 128), ([40], [5000], 64), ([100], [700], 256)])
+def test_values_at_the_types_end(counts, lens, hd):
+    """All values are float16's largest.  Every 32nd key scores one more (in log2, less a little) than the others, whose
+    weight lies just above the middle of two float16 numbers and is rounded up by 7/8 of half a step, 2^-11 of itself:
+    the mean of these values must not become infinite by that."""
+    from tests.test_gpu_attn_paged import _case, _check
+    c = _case(counts, lens, 4, 2, hd, 16)
+    pages, page = c["kp"].shape[:2]
+    c["q"].zero_()
+    c["kp"].zero_()
+    c["q"][:, :, 0] = 1
+    for b, L in enumerate(lens):
+        for t in range(0, L, 32):
+            c["kp"][R.page_of(c["tab"], pages, page, b, t), t % page, :, 0] = 1
+    c["vp"].fill_(65504)
+    c["vp"][..., 1::2] = -65504
+    scale = (1 - np.log2(1 + 2.0 ** -11 * (1 + 2.0 ** -3))) * np.log(2.0)
+    got, lse = _check(c, scale=float(np.float32(scale)))
+    assert torch.isfinite(got).all()
