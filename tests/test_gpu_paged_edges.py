@@ -124,3 +124,73 @@ def test_values_at_the_types_end(counts, lens, hd):
     scale = (1 - np.log2(1 + 2.0 ** -11 * (1 + 2.0 ** -3))) * np.log(2.0)
     got, lse = _check(c, scale=float(np.float32(scale)))
     assert torch.isfinite(got).all()
+
+
+@pytest.mark.parametrize("counts,lens,Hq,Hkv,hd,page,dtype,window", [
+    ([1], [700], 40, 1, 128, 16, "f16", 0),                       # one token, more heads than a few-row workgroup's queries
+    ([1, 1, 0, 1], [3000, 5, 9, 64], 64, 1, 64, 8, "bf16", 0),
+    ([9, 1, 3], [500, 40, 3], 16, 4, 128, 16, "f16", 0),          # nine drafts of a group of four: 36 queries a key head
+    ([1, 2], [900, 1200], 140, 1, 64, 32, "f16", 100),            # a token's heads in two workgroups
+    ([1] * 70, [1 + 13 * b for b in range(70)], 66, 2, 64, 16, "bf16", 0),
+])
+def test_large_groups(counts, lens, Hq, Hkv, hd, page, dtype, window):
+    """More than 32 queries per key head of very few tokens."""
+    from tests.test_gpu_attn_paged import _case, _check
+    _check(_case(counts, lens, Hq, Hkv, hd, page, dtype), window)
+
+
+@pytest.mark.parametrize("lens,cap,Hkv,hd,d,K,M,page,held,rope", [
+    ([900, 0, 30], 900, 2, 64, 8, 256, 2, 16, "f16", True),           # two stages resident in LDS
+    ([600], 610, 3, 64, 16, 128, 2, 32, "bf16", True),                # the same, 7-bit codes across words
+    ([600, 70], 600, 2, 128, 8, 8, 1, 16, "f16", True),               # one stage of 3-bit codes
+    ([530], 530, 2, 256, 16, 32, 1, 8, "bf16", True),                 # of 5-bit codes, heads of 256
+    ([77], 80, 5, 64, 8, 128, 1, 16, "f16", False),                   # of 7-bit codes, heads of 64
+    ([641, 640, 5, 0], 641, 8, 128, 8, 256, 2, 16, "f16", True),      # chunks of 640 tokens, a code of its own each lane
+    ([641, 100, 639, 64], 641, 8, 128, 16, 256, 4, 32, "bf16", True),  # the same, four lanes a code
+    ([700, 1290], 1290, 8, 256, 64, 64, 6, 16, "bf16", True),         # 6-bit codes, heads of 256
+])
+def test_restore_layouts(lens, cap, Hkv, hd, d, K, M, page, held, rope):
+    """Code layouts that run kernels of their own, within the tolerance derived in test_gpu_paged.test_restore."""
+    from tests.test_gpu_paged import test_restore
+    test_restore(lens, cap, Hkv, hd, d, K, M, page, held, rope)
+
+
+@pytest.mark.parametrize("d,M", [(8, 1), (8, 2), (128, 12)])
+def test_captured_restore_and_another_stream(d, M):
+    """A restore captured and replayed on changed codes and lengths, among eager work, and on a stream of its own."""
+    Hkv, hd, page, Bn, cap = 2, 128, 16, 2, 700
+    G, per = Hkv * hd // d, -(-cap // page)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    book = [torch.rand((M, G, 256), generator=g, device="cuda"), torch.randn((M, G, 256, d), generator=g, device="cuda")]
+    codes = torch.randint(-2 ** 31, 2 ** 31 - 1, (Bn, cap, M * G * 8 // 32), generator=g, device="cuda", dtype=torch.int32)
+    lens = torch.tensor([700, 333], dtype=torch.int32, device="cuda")
+    tab = R.table(Bn, per, Bn * per).cuda()
+    theta = (500000.0 ** (torch.arange(hd // 2, dtype=torch.float64) * (-2.0 / hd))).cuda()
+
+    def pools():
+        return [torch.zeros((Bn * per, page, Hkv, hd), dtype=torch.float16, device="cuda") for _ in range(2)]
+
+    def restore(kp, vp, **kw):
+        B.paged_restore(codes, codes, lens, *book, *book, kp, vp, tab, theta=theta, **kw)
+
+    kept = pools()
+    restore(*kept)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        restore(*kept)
+    side = torch.cuda.Stream()
+    for i in range(3):
+        codes.copy_(torch.randint(-2 ** 31, 2 ** 31 - 1, codes.shape, generator=g, device="cuda", dtype=torch.int32))
+        lens.sub_(torch.tensor([37, -41], dtype=torch.int32, device="cuda"))
+        for pool in kept:
+            pool.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        now, other = pools(), pools()
+        restore(*now)
+        side.wait_stream(torch.cuda.current_stream())
+        restore(*other, stream=side)
+        torch.cuda.synchronize()
+        for a, b, c in zip(kept, now, other):
+            assert torch.equal(a, b) and torch.equal(a, c) and a.any()
