@@ -660,8 +660,11 @@ def paged_append(k, v, k_pages, v_pages, table, q_start, seq_len, *, q=None, the
     seq_len [B] int32 (seq_len with the new tokens).  theta [head_dim / 2]
     float64: angle per position, e.g. base ** (-2 * arange(hd / 2) / hd); keys
     and queries are turned by it.  k_norm, q_norm [head_dim] float32.
-    Returns the queries [T, Hq, head_dim] in the pages' type, or None
-    without q."""
+    Returns the queries [T, Hq, head_dim] in the pages' type (q_out, or a new
+    tensor in which rows of no sequence hold anything), or None without q.
+    Keys that are also coded (encode, float16 or float32 rows) are coded after
+    their norm, which the caller applies for it, and before the rotation:
+    paged_restore turns them and norms nothing."""
     torch = _torch()
     lib = _lib or load_library()
     pages = _pages(k_pages, v_pages, table)
@@ -717,8 +720,9 @@ def attn_paged(q, k_pages, v_pages, table, q_start, seq_len, *, scale=None, wind
     """Causal attention of new tokens over their sequences' pages (see
     gsrq_attn_paged), after paged_append of the same rows.  q [T, Hq, head_dim]
     of the pages' type, any strides.  Returns out [T, Hq, head_dim] of the
-    same type, with lse=True also the rows' log-sum-exp [T, Hq] float32.
-    workspace: a uint8 tensor of attn_paged_workspace_bytes, or None (one is
+    same type (apart from q; rows of no sequence are left as they are, in a
+    new tensor anything), with lse=True also the rows' log-sum-exp [T, Hq]
+    float32.  workspace: a uint8 tensor of attn_paged_workspace_bytes, or None (one is
     made for the call)."""
     torch = _torch()
     lib = _lib or load_library()
@@ -770,7 +774,8 @@ def paged_restore(k_codes, v_codes, seq_len, k_gain, k_shape, v_gain, v_shape, k
     """Decode coded contexts into pages (see gsrq_paged_restore): k_codes,
     v_codes [B, cap, W] packed codes, seq_len [B] int32, codebooks [M, G, K]
     and [M, G, K, d]; the pages, the table and theta as paged_append takes
-    them."""
+    them.  Keys: as they were before the rotation, normed if the model norms
+    its keys."""
     torch = _torch()
     lib = load_library()
     pages = _pages(k_pages, v_pages, table)
