@@ -403,8 +403,8 @@ gsrq_status gsrq_attn_decode_noalloc(const gsrq_attn_shape* a, const gsrq_shape*
  * and [pages][Hkv][page_size][head_dim] are both taken.  A table entry outside
  * [0, pages) stands for a page that is not there: nothing is written to its
  * tokens, and nobody attends to them.  A page may stand in several rows of the
- * table (a shared prompt); a call that writes one token of a page from two
- * rows leaves either.
+ * table (a shared prompt); of a token that a call writes from two rows every
+ * eight elements are one of the rows'.
  * This build: head_dim 64, 128 or 256, page_size a power of two from 8 on,
  * float16 or bfloat16 pages, tokens less than 2^26 and pages less than 2^31
  * elements apart (other valid shapes GSRQ_E_UNSUPPORTED); per * page_size at
@@ -497,14 +497,19 @@ gsrq_status gsrq_attn_paged_workspace_bytes(const gsrq_paged_attn* s, const gsrq
  * infinity or NaN among the values that it sees does, however small its weight.
  *
  *  q                 [T][Hq][head_dim] rows of the pages' type, turned.
- *  out               [T][Hq][head_dim] of the pages' type, 16-byte aligned.
+ *  out               [T][Hq][head_dim] of the pages' type, 16-byte aligned; no
+ *                    part of q or of the pages.
  *  lse               [T][Hq] float32, or NULL.
  *  workspace         >= gsrq_attn_paged_workspace_bytes(s, pages), 256-byte
  *                    aligned; nothing is kept in it between calls.
  * Precision: products of the pages' type with float32 sums; softmax weights
- * are rounded to the pages' type for the product with the values; maxima,
- * sums and the joining of pieces are float32.  The result does not depend on
- * the order in which the GPU runs the work.
+ * are rounded to the pages' type for the product with the values, while their
+ * sum (and lse) has them unrounded; maxima, sums and the joining of pieces are
+ * float32.  In float16 a weight below about 2^-31 of the largest counts in the
+ * sum alone: the values of n such tokens, up to n 2^-31 of all weight, are
+ * missing from a result (n = 10^6: about a rounding of float16).  Scores
+ * scale q.k are below 2^23 in size and bfloat16 values below 2^96.  The result
+ * does not depend on the order in which the GPU runs the work.
  */
 gsrq_status gsrq_attn_paged(const gsrq_paged_attn* s, const gsrq_pages* pages,
                             const int32_t* q_start, const int32_t* seq_len, const gsrq_heads* q,
@@ -514,14 +519,16 @@ gsrq_status gsrq_attn_paged(const gsrq_paged_attn* s, const gsrq_pages* pages,
  * gsrq_paged_restore -- decode a coded context into pages: tokens
  * 0 .. seq_len[b] - 1 of every sequence, values as gsrq_decode gives them and
  * keys turned at their positions by theta as gsrq_paged_append does (keys are
- * coded before their rotation).  Each stage's codeword is rounded to float32,
+ * coded after the norm of their heads, if they have one, and before their
+ * rotation).  Each stage's codeword is rounded to float32,
  * the stages are summed in float32 in stage order, and the result (keys:
  * after a float32 rotation) is rounded once to the pages' type.
  *
  *  kv                code shape: D = Hkv * head_dim, d >= 8, any K, M that
  *                    gsrq_decode takes.
  *  cap               code rows per sequence, at most 2^30; seq_len is held
- *                    inside [0, cap].
+ *                    inside [0, cap].  B * cap, Hkv and head_dim whose launch
+ *                    would pass 2^32 threads: GSRQ_E_UNSUPPORTED.
  *  k_codes, v_codes  [B][cap][gsrq_code_words(kv)] uint32 (kv->N >= B * cap).
  *  seq_len           [B] int32.
  *  k_gain, k_shape   codebooks [M][G][K], [M][G][K][d], shapes 16-byte aligned.
