@@ -1023,8 +1023,8 @@ __device__ __forceinline__ int few_parts(const PtArgs& a, const Seq& s) {
 // One wave (shared: one workgroup) per row and head (and, where the records of
 // the `few` kind are laid out by sequence, one per such record).  A row's
 // records are found without its sequence, so their first loads are on their
-// way while the sequence is looked up (three round trips to memory one after
-// the other before: 4.4 -> 2.7 us for one token's rows).
+// way while the sequence is looked up, not after three round trips to memory
+// one after the other (one token's rows: 3.9 us).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) paged_attn_merge_kernel(PtArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1100,7 +1100,10 @@ gsrq_status pt_plan(const gsrq_paged_attn* s, const gsrq_pages* pages, PtPlan& p
   // at the least.  More, shorter ones cost their starts: 8 sequences of 2048
   // tokens took 25 us in 1024 workgroups, 19 in 512.  Four pieces at the
   // least where the sequences alone would fill the GPU: one of them may be much
-  // longer than the others.  None where the table holds 256 tokens at most: 8 us
+  // longer than the others (128 sequences of 8 heads, one of 20000 tokens among
+  // 500s: 146 us with one piece, 99 with four, 104 with 16).  A fixed number
+  // cannot follow every batch: one of 100000 among 31 of 1000 takes 296 us in
+  // these four and 123 in 16, 32 of 4000 take 101 and 117.  None where the table holds 256 tokens at most: 8 us
   // a call against 10 with the joining launch; at 700 tokens 16 against 11.
   int64_t few = 1;
   if (cap > 256) {

@@ -261,7 +261,7 @@ __device__ __forceinline__ char* token_at(const RestoreArgs& a, const Slice& s, 
 // and the 8 they are turned with: two codes and four 16-byte gathers a stage.
 // L = 8 for heads of 128 and more, so that a workgroup writes whole 128-byte
 // lines (L = 4, 64-byte pieces of a line from two workgroups: 182 us against
-// 129 for 4 x <= 32768 tokens x 1024 of 1 bit, of which 66 without the
+// 129 for 4 x <= 32768 tokens x 1024 of 1 bit, of which 67 without the
 // stores).  The four groups of columns of an LDS row are permuted by the
 // codeword's index, so that tokens' gathers, which want the same columns, meet
 // less in a bank.  Angles: position = chunk + 128 slot + row; the row's rotation
@@ -615,7 +615,12 @@ template <typename TP> gsrq_status restore_launch(const RestoreArgs& a, hipStrea
   }
   if (near && a.K <= PS_K) {
     // chunks of 640 tokens (fewer fills of the stages' buffers) where they
-    // give every CU a workgroup, else of 128
+    // give every CU a workgroup, else of 128, which start more workgroups on few
+    // tokens.  One sequence, 8 heads of 128, 12 stages, chunks of 128 against
+    // 640: 600 tokens 14 us and 20, 1280 tokens 27 and 21, 5100 tokens (256 long
+    // chunks) 61 and 22.  Long chunks win before that where the cache is full,
+    // but `cap` is all that is known here: three sequences of 460 to 1387
+    // tokens, 2 heads, took 14 us and 20.
     constexpr int LONG = 10, SHORT = 2;
     const int64_t longs = nsub * B * ((a.cap + PS_ROWS * LONG - 1) / (PS_ROWS * LONG));
     const int64_t shorts = nsub * B * ((a.cap + PS_ROWS * SHORT - 1) / (PS_ROWS * SHORT));

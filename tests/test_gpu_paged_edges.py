@@ -194,3 +194,22 @@ def test_captured_restore_and_another_stream(d, M):
         torch.cuda.synchronize()
         for a, b, c in zip(kept, now, other):
             assert torch.equal(a, b) and torch.equal(a, c) and a.any()
+
+
+def test_restored_tokens_do_not_depend_on_the_chunks():
+    """Chunks of 128 tokens in a short cache and of 640 in a long one give a token the same bits, rotation included."""
+    Hkv, hd, page, d, M, n = 8, 128, 16, 128, 3, 700
+    g = torch.Generator(device="cuda").manual_seed(5)
+    book = [torch.rand((M, Hkv, 256), generator=g, device="cuda"), torch.randn((M, Hkv, 256, d), generator=g, device="cuda")]
+    codes = torch.randint(-2 ** 31, 2 ** 31 - 1, (1, 9000, M * Hkv // 4), generator=g, device="cuda", dtype=torch.int32)
+    theta = (500000.0 ** (torch.arange(hd // 2, dtype=torch.float64) * (-2.0 / hd))).cuda()
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    tab = torch.arange(-(-n // page), dtype=torch.int32, device="cuda")[None]
+    got = []
+    for cap in (n, 1300, 9000):
+        kp, vp = (torch.zeros((tab.numel(), page, Hkv, hd), dtype=torch.float16, device="cuda") for _ in range(2))
+        c = codes[:, :cap].contiguous()
+        B.paged_restore(c, c, lens, *book, *book, kp, vp, tab, theta=theta)
+        got.append((kp, vp))
+    for kp, vp in got[1:]:
+        assert torch.equal(kp, got[0][0]) and torch.equal(vp, got[0][1]) and kp.any()
