@@ -275,7 +275,8 @@ template <typename T, int HD> struct Columns {
   int all_lo, all_hi;             // keys that every query of the wave sees
 
   // Query r of the sequence.  Rows past the last are copies of row 0 that see
-  // everything, so that they ask for no masks; what they come to is not used.
+  // everything, so that they ask for no masks; what they come to (weights of
+  // zero, or NaN) is not used.
   __device__ __forceinline__ void start(const PtArgs& a, const Seq& s, int head, int r) {
     const int half = (threadIdx.x >> 5) & 1;
     const bool real = r < s.n * a.GQ;
@@ -309,7 +310,7 @@ template <typename T, int HD> struct Columns {
     for (int t = 0; t < DT; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-    m = -INFINITY;
+    m = real ? -INFINITY : INFINITY;                   // (a copy's maximum is never raised)
     l = 0.f;
   }
 
@@ -354,11 +355,12 @@ template <typename T, int HD> struct Columns {
     if (NB > 1) top = fmaxf(top, max16(sc[NB - 1]));
     const float2 tops = both_halves(top);
     top = fmaxf(tops.x, tops.y) * a.c;
-    if (__any(top > m + PT_HEADROOM)) {
-      const float now = fmaxf(m, top);
-      // (a query that has seen nothing keeps -inf)
-      const float f = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
-      m = now;
+    // (each query by itself: what another one sees changes no bit of its result;
+    // one that has seen nothing keeps -inf)
+    const bool past = top > m + PT_HEADROOM;
+    if (__any(past)) {
+      const float f = past ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+      m = past ? top : m;
       l *= f;
 #pragma unroll
       for (int t = 0; t < DT; ++t)
@@ -1103,8 +1105,9 @@ gsrq_status pt_plan(const gsrq_paged_attn* s, const gsrq_pages* pages, PtPlan& p
   // longer than the others (128 sequences of 8 heads, one of 20000 tokens among
   // 500s: 146 us with one piece, 99 with four, 104 with 16).  A fixed number
   // cannot follow every batch: one of 100000 among 31 of 1000 takes 296 us in
-  // these four and 123 in 16, 32 of 4000 take 101 and 117.  None where the table holds 256 tokens at most: 8 us
-  // a call against 10 with the joining launch; at 700 tokens 16 against 11.
+  // these four and 123 in 16, 32 of 4000 take 101 and 117.  None where the table
+  // holds 256 tokens at most: 8 us a call against 10 with the joining launch; at
+  // 700 tokens 16 against 11.
   int64_t few = 1;
   if (cap > 256) {
     const int64_t once = (512 + B * Hkv - 1) / (B * Hkv);

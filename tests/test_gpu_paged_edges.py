@@ -213,3 +213,36 @@ def test_restored_tokens_do_not_depend_on_the_chunks():
         got.append((kp, vp))
     for kp, vp in got[1:]:
         assert torch.equal(kp, got[0][0]) and torch.equal(vp, got[0][1]) and kp.any()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("counts,lens,hd,window", [([1, 6], [77, 700], 128, 0), ([7], [133], 64, 40), ([4, 6], [500, 640], 256, 0),
+                                                   ([90, 150], [90, 333], 128, 0), ([200], [300], 64, 70), ([70], [201], 256, 0)])
+def test_what_a_row_does_not_see_changes_no_bit(counts, lens, hd, window, dtype):
+    """Keys and values behind a sequence's end, in absent pages' places and, for the first rows of a call, in the tokens
+    after theirs: large and small ones give the same bits, on keys that grow along the sequence, so that the maximum in
+    use lags behind the largest score by up to 2^8."""
+    from tests.test_gpu_attn_paged import ORDER, _case
+    c = _case(counts, lens, 8, 2, hd, 16, dtype)
+    pages, page = c["kp"].shape[:2]
+    grow = torch.linspace(0.5, 2.0, max(lens)).to(c["kp"].dtype)
+    used = torch.zeros((pages, page), dtype=torch.bool)
+    late = []
+    for b, L in enumerate(lens):
+        for t in range(L):
+            at = R.page_of(c["tab"], pages, page, b, t)
+            used[at, t % page] = True
+            c["kp"][at, t % page] *= grow[t]
+        late += [(R.page_of(c["tab"], pages, page, b, t), t % page) for t in range(L - counts[b] // 2, L)]
+    got = []
+    for size in (0.0, 1.0, 30.0, -30.0):
+        d = {n: c[n].clone() for n in ORDER}
+        for name in ("kp", "vp"):
+            d[name][~used] = size
+            for at, i in late:
+                d[name][at, i] = size
+        got.append([x.cpu() for x in B.attn_paged(*(d[n].cuda() for n in ORDER), window=window, lse=True)])
+    for b, n in enumerate(counts):
+        first = slice(int(c["start"][b]), int(c["start"][b]) + n - n // 2)
+        for other in got[1:]:
+            assert torch.equal(other[0][first], got[0][0][first]) and torch.equal(other[1][first], got[0][1][first])
