@@ -51,8 +51,10 @@ typedef enum {
   GSRQ_E_HIP = 4           /* a HIP runtime call failed                    */
 } gsrq_status;
 
-/* GSRQ_BF16: the paged cache's entry points only. */
-typedef enum { GSRQ_F32 = 0, GSRQ_F16 = 1, GSRQ_BF16 = 2 } gsrq_dtype;
+/* GSRQ_BF16: the paged cache's entry points and gsrq_verify_drafts only;
+ * GSRQ_E4M3 (8 bits: sign, 4 of exponent, 3 of mantissa; 448 at most, no
+ * infinities, 0x7f and 0xff NaN): the codes of 8-bit pages only. */
+typedef enum { GSRQ_F32 = 0, GSRQ_F16 = 1, GSRQ_BF16 = 2, GSRQ_E4M3 = 3 } gsrq_dtype;
 
 /* Problem shape.  N rows of D elements, subvector dimension d (d divides D,
  * G = D/d subspaces), K codewords per codebook (power of two), M stages. */
@@ -516,6 +518,79 @@ gsrq_status gsrq_attn_paged(const gsrq_paged_attn* s, const gsrq_pages* pages,
                             void* out, float* lse, void* workspace, size_t ws_bytes, void* stream);
 
 /*
+ * 8-bit pages: a pool of codes (gsrq_pages with dtype GSRQ_E4M3, one byte an
+ * element, pools 16-byte aligned and strides multiples of 16) and, for every
+ * page and key/value head, the exponent of a scale: a code c of page g and
+ * head h stands for c * 2^e, e = k[g * k_stride[0] + h * k_stride[1]] (values
+ * from v).  A scale that is a power of two lets a page's codes move to a larger
+ * one without a rounding of their own, but for those that fall below the
+ * smallest normal code.  Exponents that gsrq_paged_append8 writes lie between
+ * GSRQ_EXP_MIN and GSRQ_EXP_MAX; others count as the nearer of the two.
+ */
+#define GSRQ_EXP_MIN (-40)
+#define GSRQ_EXP_MAX 40
+typedef struct {
+  int8_t* k;               /* [pages][Hkv] exponents of the key pages, at any  */
+  int8_t* v;               /* strides, and of the value pages                  */
+  int64_t k_stride[2];     /* elements from page to page and head to head      */
+  int64_t v_stride[2];
+} gsrq_page_exps;
+
+/*
+ * gsrq_paged_append8 -- gsrq_paged_append into 8-bit pages.  Rows, positions,
+ * norms and rotations are the same; what is stored differs.  For a page and
+ * head that get new tokens, with a the largest finite size among the new
+ * tokens' elements there (after norm and rotation),
+ *   e = min { e >= GSRQ_EXP_MIN : a <= 448 * 2^e }, at most GSRQ_EXP_MAX,
+ * and at least the exponent before unless the page's first token is among
+ * the new ones (the page starts anew).  New elements x become the code nearest
+ * to x * 2^-e, ties to even (beyond 448: +-448; infinities and NaN: NaN).  Where the
+ * exponent has risen, the codes of the tokens before the new ones are
+ * rounded again to the new scale; codes of later places stay as they are.  The
+ * exponent is that of 64-bit norms and rotations; codes are rounded from
+ * float32.  Tokens taken back (drafts that were rejected) leave the exponent
+ * where they have raised it.
+ *
+ * A page that a call writes from two rows of the table holds anything
+ * afterwards.
+ *
+ *  q_out, q_dtype    queries [T][Hq][head_dim], float16 or bfloat16.
+ *  other arguments   as gsrq_paged_append.
+ */
+gsrq_status gsrq_paged_append8(const gsrq_pages* pages, const gsrq_page_exps* exps, int64_t T,
+                               const int32_t* q_start, const int32_t* seq_len,
+                               const gsrq_heads* k, const gsrq_heads* v, const gsrq_heads* q,
+                               int32_t Hq, gsrq_dtype dtype, const double* theta,
+                               const float* k_norm, const float* q_norm, float eps, void* q_out,
+                               gsrq_dtype q_dtype, void* stream);
+
+/* Workspace bytes gsrq_attn_paged8 needs (0: none). */
+gsrq_status gsrq_attn_paged8_workspace_bytes(const gsrq_paged_attn* s, const gsrq_pages* pages,
+                                             size_t* bytes);
+
+/*
+ * gsrq_attn_paged8 -- gsrq_attn_paged over 8-bit pages: the same rows, masks,
+ * results and workspace rules, with k_j and v_j the values that codes and
+ * exponents stand for.
+ *
+ *  q, q_dtype        [T][Hq][head_dim] rows of float16 or bfloat16, turned.
+ *  out               [T][Hq][head_dim] of that type, 16-byte aligned.
+ * Precision: codes enter the products as they are (each is a number of either
+ * type); a page's key scale multiplies float32 scores, its value scale the
+ * weights before they are rounded to the queries' type, relative to the
+ * largest product of weight and scale; maxima, sums and the joining of pieces
+ * are float32.  In float16 a product of weight and scale below about 2^-31 of
+ * the largest is missing from a result's values.  float16 results beyond
+ * 65504 are held there.  A NaN code that a row sees reaches it.  What a row does
+ * not see reaches it only through the exponent of a page that it sees in part.
+ */
+gsrq_status gsrq_attn_paged8(const gsrq_paged_attn* s, const gsrq_pages* pages,
+                             const gsrq_page_exps* exps, const int32_t* q_start,
+                             const int32_t* seq_len, const gsrq_heads* q, gsrq_dtype q_dtype,
+                             void* out, float* lse, void* workspace, size_t ws_bytes,
+                             void* stream);
+
+/*
  * gsrq_paged_restore -- decode a coded context into pages: tokens
  * 0 .. seq_len[b] - 1 of every sequence, values as gsrq_decode gives them and
  * keys turned at their positions by theta as gsrq_paged_append does (keys are
@@ -541,6 +616,91 @@ gsrq_status gsrq_paged_restore(const gsrq_pages* pages, const gsrq_shape* kv, in
                                const float* v_gain, const float* v_shape, const double* theta,
                                void* stream);
 
+/* Shape of a batch whose requests' lengths change. */
+typedef struct {
+  int64_t T;          /* rows that slots and positions have room for          */
+  int64_t ldt;        /* entries from row to row of the table (>= per)        */
+  int32_t B;          /* sequences, at most 8192                              */
+  int32_t per;        /* table entries per sequence                           */
+  int32_t page_size;  /* tokens per page (as gsrq_pages)                      */
+  int32_t F;          /* entries of the free list: as many as the pool's pages */
+} gsrq_paged_batch;
+
+/*
+ * gsrq_paged_plan -- what gsrq_paged_append and gsrq_attn_paged take, from the
+ * requests' lengths: sequence b brings change[b] new tokens, or (below zero)
+ * gives that many back, and its pages come from or go to a list of free ones.
+ * With L = seq_len[b] and L' = max(L + change[b], 0):
+ *  1. A sequence that shrinks gives back the pages of its table row past
+ *     ceil(L' / page_size); their entries become -1.  All pages given back go on
+ *     the list in an order in which the same sequences, growing again, would
+ *     get them again.  Entries below zero (absent pages) are left out.  The
+ *     page of a token that stays is kept.
+ *  2. The sequences that grow are served in order of b, from the end of the
+ *     list, as long as the pages and rows asked for up to and with b are there;
+ *     the entries taken become -1.  One that asks for more than its table row
+ *     holds (L' > per * page_size) is passed over and asks for nothing.
+ *  3. q_start[b] counts the new tokens of the served sequences before b, and
+ *     seq_len[b] becomes L' for them and those that shrink.  A sequence that
+ *     was not served has no rows and keeps its length.
+ *  4. Row q_start[b] + i is at position p = L + i: slots[row] = page *
+ *     page_size + p % page_size, its place among a dense pool's tokens, and
+ *     positions[row] = p.  Rows of no sequence, up to T, get -1 in both.
+ *
+ *  table             [B][ldt] int32, in and out; entries past a sequence's
+ *                    pages are neither read nor kept.
+ *  free_pages        [F] int32, in and out: the first n_free[0] are free (held
+ *                    inside [0, F]); pages given back beyond F are dropped.
+ *  n_free            [1] int32, in and out.
+ *  seq_len           [B] int32, in and out (held inside [0, per * page_size]).
+ *  change            [B] int32.
+ *  q_start           [B + 1] int32.
+ *  slots, positions  [T] int64, [T] int32 (NULL where T is 0).
+ * A page that stands in several rows of the table is given back by each: the
+ * caller counts shared pages.  No array overlaps another.
+ */
+gsrq_status gsrq_paged_plan(const gsrq_paged_batch* s, int32_t* table, int32_t* free_pages,
+                            int32_t* n_free, int32_t* seq_len, const int32_t* change,
+                            int32_t* q_start, int64_t* slots, int32_t* positions, void* stream);
+
+/* Workspace bytes gsrq_verify_drafts needs. */
+gsrq_status gsrq_verify_drafts_workspace_bytes(int64_t T, int64_t V, int32_t B, size_t* bytes);
+
+/*
+ * gsrq_verify_drafts -- which of the drafted tokens of every sequence stand
+ * (speculative sampling with given random numbers), and the token after them.
+ * Rows are those of an attention call: sequence b's are the token before its
+ * drafts and the drafts, in order, and row r's probabilities are for the token
+ * of row r + 1.  With p and q the target's and the draft's probabilities of
+ * row r, draft t = tokens[r + 1] is accepted iff uniform[r] * q(t) < p(t); the
+ * first that is not ends the sequence's drafts.  The next token is drawn from
+ *   w(v) = max(p(v) - q(v), 0)    of the row of the rejected draft
+ *                                 (from p where that is zero everywhere),
+ *   w(v) = p(v)                   of the last row, where none was rejected:
+ * the lowest v with w(0) + .. + w(v) > draw[b] * sum of w, or, where there is none,
+ * the last v of a weight above zero.  Sums and products are float64.  Weights below
+ * zero and NaN count as zero; a token outside [0, V) has p = q = 0.
+ *
+ *  tokens            [T] int32; a sequence's first is not looked at.
+ *  target            [T][ldp] probabilities of `dtype` (float32, float16,
+ *                    bfloat16), ldp >= V; need not sum to one.
+ *  draft             [T][ldq], or NULL: drafts were chosen without chance, q is
+ *                    1 for a draft and 0 for every other token.  A sequence's
+ *                    last row is not looked at.
+ *  uniform, draw     [T], [B] float32 numbers of [0, 1).
+ *  q_start           [B + 1] int32, ascending, inside [0, T].
+ *  accepted          [B] int32: drafts accepted (0 for a sequence without rows).
+ *  next              [B] int32: the token after them; -1 for a sequence without
+ *                    rows and where no weight is above zero.
+ *  workspace         >= gsrq_verify_drafts_workspace_bytes(T, V, B), 256-byte
+ *                    aligned.
+ */
+gsrq_status gsrq_verify_drafts(int64_t T, int64_t V, int32_t B, const int32_t* tokens,
+                               const void* target, int64_t ldp, const void* draft, int64_t ldq,
+                               gsrq_dtype dtype, const float* uniform, const float* draw,
+                               const int32_t* q_start, int32_t* accepted, int32_t* next,
+                               void* workspace, size_t ws_bytes, void* stream);
+
 /* Kernel kinds reported by the optional launch timing below. */
 enum {
   GSRQ_KERNEL_ASSIGN = 0,     /* fused assignment + weighted accumulation */
@@ -555,7 +715,8 @@ enum {
   GSRQ_KERNEL_EXACT = 7,      /* float64 rescoring of deferred rows         */
   GSRQ_KERNEL_ATTENTION = 8,  /* attention over a coded or paged cache     */
   GSRQ_KERNEL_APPEND = 9,     /* appending to a paged cache                */
-  GSRQ_KERNEL_KINDS = 10
+  GSRQ_KERNEL_SERVING = 10,   /* planning of a batch's pages, drafts         */
+  GSRQ_KERNEL_KINDS = 11
 };
 
 /* Measurement hook, the library's only process state.  While enabled, every

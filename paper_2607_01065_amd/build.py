@@ -7,7 +7,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SRCS = [os.path.join(HERE, "csrc", f) for f in ("gsrq.hip", "gsrq_wide.hip", "gsrq_weights.hip", "gsrq_attn.hip",
-                                                  "gsrq_paged.hip", "gsrq_attn_paged.hip")]
+                                                  "gsrq_paged.hip", "gsrq_attn_paged.hip",
+                                                  "gsrq_cache8.hip", "gsrq_serving.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libgsrq.so")
 
@@ -37,6 +38,7 @@ def hipcc():
 SRC_FLAGS = {
     "gsrq_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "gsrq_attn_paged.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "gsrq_cache8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "gsrq.hip": ["-mllvm", "-amdgpu-atomic-optimizer-strategy=None"],
 }
 

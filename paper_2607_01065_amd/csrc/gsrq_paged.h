@@ -25,12 +25,13 @@ struct PagePool {
   int pages, shift, per, B, Hkv;
 };
 
-// Host checks of a pool (no HIP call).
-inline gsrq_status page_pool(const gsrq_pages* p, PagePool& o) {
+// Host checks of a pool (no HIP call), of 8-bit pages or of 16-bit ones.
+inline gsrq_status page_pool(const gsrq_pages* p, bool eight, PagePool& o) {
   if (!p || !p->k || !p->v || !p->table) return GSRQ_E_ARG;
   if (p->pages < 1 || p->page_size < 1 || p->per < 1 || p->B < 1 || p->Hkv < 1) return GSRQ_E_ARG;
   if (p->ldt < p->per || p->head_dim < 1) return GSRQ_E_ARG;
-  if (p->dtype != GSRQ_F16 && p->dtype != GSRQ_BF16)
+  if (eight && p->dtype != GSRQ_E4M3) return GSRQ_E_ARG;
+  if (!eight && p->dtype != GSRQ_F16 && p->dtype != GSRQ_BF16)
     return p->dtype == GSRQ_F32 ? GSRQ_E_UNSUPPORTED : GSRQ_E_ARG;
   if ((int64_t)p->page_size * p->per > (1 << 30)) return GSRQ_E_ARG;
   if (p->head_dim != 64 && p->head_dim != 128 && p->head_dim != 256) return GSRQ_E_UNSUPPORTED;
@@ -43,7 +44,7 @@ inline gsrq_status page_pool(const gsrq_pages* p, PagePool& o) {
   for (int i = 0; i < 3; ++i) {
     const int64_t least = count[i] > 1 ? 1 : 0;      // no two tokens in one place
     if (p->k_stride[i] < least || p->v_stride[i] < least) return GSRQ_E_ARG;
-    if (p->k_stride[i] % 8 || p->v_stride[i] % 8) return GSRQ_E_ARG;
+    if (p->k_stride[i] % (eight ? 16 : 8) || p->v_stride[i] % (eight ? 16 : 8)) return GSRQ_E_ARG;
     o.ks[i] = p->k_stride[i];
     o.vs[i] = p->v_stride[i];
   }
@@ -108,6 +109,44 @@ __device__ __forceinline__ int sequence_of(const int32_t* q_start, int B, int ro
   }
   b = __builtin_amdgcn_readfirstlane(b);
   return b < B && q_start[b] <= row ? b : -1;
+}
+
+// Eight elements of a row, in float32.
+__device__ __forceinline__ void load8(const _Float16* p, float (&x)[8]) {
+  const h8 v = *(const h8*)p;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
+}
+__device__ __forceinline__ void load8(const __bf16* p, float (&x)[8]) {
+  const b8 v = *(const b8*)p;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
+}
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+  const f4 lo = ((const f4*)p)[0], hi = ((const f4*)p)[1];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) { x[j] = lo[j]; x[4 + j] = hi[j]; }
+}
+// Rounded to the pages' type here, once (to the nearest, ties to even).
+__device__ __forceinline__ void store8(_Float16* p, const float (&x)[8]) {
+  h8 v;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = (_Float16)x[j];
+  *(h8*)p = v;
+}
+__device__ __forceinline__ void store8(__bf16* p, const float (&x)[8]) {
+  b8 v;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = (__bf16)x[j];
+  *(b8*)p = v;
+}
+
+// Cosine and sine of pos * theta.  In 64 bits up to the whole turns: at
+// position 2^20 a float32 product would be off by 0.06 radians.
+__device__ __forceinline__ void turn_of(int64_t pos, double theta, float& c, float& s) {
+  double r = (double)pos * (theta * 0.15915494309189533577);   // 1 / (2 pi)
+  r -= rint(r);
+  sincospif(2.f * (float)r, &s, &c);
 }
 
 }  // namespace

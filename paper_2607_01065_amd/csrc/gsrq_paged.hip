@@ -20,43 +20,6 @@ namespace {
 
 constexpr int PA_THREADS = 256;
 
-__device__ __forceinline__ void load8(const _Float16* p, float (&x)[8]) {
-  const h8 v = *(const h8*)p;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
-}
-__device__ __forceinline__ void load8(const __bf16* p, float (&x)[8]) {
-  const b8 v = *(const b8*)p;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
-}
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const f4 lo = ((const f4*)p)[0], hi = ((const f4*)p)[1];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) { x[j] = lo[j]; x[4 + j] = hi[j]; }
-}
-// Rounded to the pages' type here, once (to the nearest, ties to even).
-__device__ __forceinline__ void store8(_Float16* p, const float (&x)[8]) {
-  h8 v;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = (_Float16)x[j];
-  *(h8*)p = v;
-}
-__device__ __forceinline__ void store8(__bf16* p, const float (&x)[8]) {
-  b8 v;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = (__bf16)x[j];
-  *(b8*)p = v;
-}
-
-// Cosine and sine of pos * theta.  In 64 bits up to the whole turns: at
-// position 2^20 a float32 product would be off by 0.06 radians.
-__device__ __forceinline__ void turn_of(int64_t pos, double theta, float& c, float& s) {
-  double r = (double)pos * (theta * 0.15915494309189533577);   // 1 / (2 pi)
-  r -= rint(r);
-  sincospif(2.f * (float)r, &s, &c);
-}
-
 struct AppendArgs {
   PagePool pool;
   const void *k, *v, *q;
@@ -659,7 +622,7 @@ gsrq_status gsrq_paged_append(const gsrq_pages* pages, int64_t T, const int32_t*
                               const double* theta, const float* k_norm, const float* q_norm,
                               float eps, void* q_out, void* stream) {
   AppendArgs a;
-  gsrq_status e = page_pool(pages, a.pool);
+  gsrq_status e = page_pool(pages, false, a.pool);
   if (e) return e;
   if (T < 1 || !q_start || !seq_len) return GSRQ_E_ARG;
   if (dtype != GSRQ_F32 && dtype != GSRQ_F16 && dtype != GSRQ_BF16) return GSRQ_E_ARG;
@@ -707,7 +670,7 @@ gsrq_status gsrq_paged_restore(const gsrq_pages* pages, const gsrq_shape* kv, in
                                const float* v_gain, const float* v_shape, const double* theta,
                                void* stream) {
   RestoreArgs a;
-  gsrq_status e = page_pool(pages, a.pool);
+  gsrq_status e = page_pool(pages, false, a.pool);
   if (e) return e;
   if (!kv || cap < 1 || kv->N < 1 || kv->D < 1 || kv->d < 1 || kv->K < 2 || kv->M < 1)
     return GSRQ_E_ARG;

@@ -20,7 +20,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libgsrq.so")
 
 GSRQ_OK, GSRQ_E_ARG, GSRQ_E_UNSUPPORTED, GSRQ_E_WORKSPACE, GSRQ_E_HIP = range(5)
-GSRQ_F32, GSRQ_F16, GSRQ_BF16 = 0, 1, 2
+GSRQ_F32, GSRQ_F16, GSRQ_BF16, GSRQ_E4M3 = 0, 1, 2, 3
 GSRQ_RESUME, GSRQ_ASSIGN_IN, GSRQ_NO_EARLY_STOP, GSRQ_KMEANS, GSRQ_CHECK_INPUTS = 1, 2, 4, 8, 16
 
 
@@ -53,6 +53,16 @@ class Pages(ctypes.Structure):
 class Heads(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
                 ("head_stride", ctypes.c_int64)]
+
+
+class PageExps(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_stride", ctypes.c_int64 * 2),
+                ("v_stride", ctypes.c_int64 * 2)]
+
+
+class PagedBatch(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("ldt", ctypes.c_int64), ("B", ctypes.c_int32),
+                ("per", ctypes.c_int32), ("page_size", ctypes.c_int32), ("F", ctypes.c_int32)]
 
 
 class PagedAttn(ctypes.Structure):
@@ -125,6 +135,25 @@ def load_library(path: str = LIB_PATH):
     lib.gsrq_paged_restore.restype = ctypes.c_int
     lib.gsrq_paged_restore.argtypes = [PP, SP, ctypes.c_int32, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                        _vp, _vp]
+    lib.gsrq_paged_append8.restype = ctypes.c_int
+    lib.gsrq_paged_append8.argtypes = [PP, _vp, ctypes.c_int64, _vp, _vp, HP, HP, HP,
+                                       ctypes.c_int32, ctypes.c_int, _vp, _vp, _vp, ctypes.c_float,
+                                       _vp, ctypes.c_int, _vp]
+    lib.gsrq_attn_paged8_workspace_bytes.restype = ctypes.c_int
+    lib.gsrq_attn_paged8_workspace_bytes.argtypes = [XP, PP, ctypes.POINTER(ctypes.c_size_t)]
+    lib.gsrq_attn_paged8.restype = ctypes.c_int
+    lib.gsrq_attn_paged8.argtypes = [XP, PP, _vp, _vp, _vp, HP, ctypes.c_int, _vp, _vp, _vp,
+                                     ctypes.c_size_t, _vp]
+    lib.gsrq_paged_plan.restype = ctypes.c_int
+    lib.gsrq_paged_plan.argtypes = [_vp] * 10
+    lib.gsrq_verify_drafts_workspace_bytes.restype = ctypes.c_int
+    lib.gsrq_verify_drafts_workspace_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64,
+                                                       ctypes.c_int32,
+                                                       ctypes.POINTER(ctypes.c_size_t)]
+    lib.gsrq_verify_drafts.restype = ctypes.c_int
+    lib.gsrq_verify_drafts.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, _vp, _vp,
+                                       ctypes.c_int64, _vp, ctypes.c_int64, ctypes.c_int, _vp,
+                                       _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
     lib.gsrq_attn_paged_workspace_bytes.restype = ctypes.c_int
     lib.gsrq_attn_paged_workspace_bytes.argtypes = [XP, PP, ctypes.POINTER(ctypes.c_size_t)]
     lib.gsrq_attn_paged.restype = ctypes.c_int
@@ -141,7 +170,7 @@ def load_library(path: str = LIB_PATH):
 
 
 KERNEL_KINDS = ("assign", "finalize", "encode", "decode", "transpose", "accumulate",
-                "fragments", "exact", "attention", "append")
+                "fragments", "exact", "attention", "append", "serving")
 
 
 def timing_enable(on: bool = True, kinds=None):
@@ -557,11 +586,13 @@ def attn_decode(k_codes, v_codes, seq_len, k_gain, k_shape, v_gain, v_shape, q, 
 # ------------------------------------------------------------- paged cache
 
 # The structures of the calls of every decoding step are packed, not built
-# field by field (a few microseconds of a call); layouts as Pages, Heads and
-# PagedAttn above.
+# field by field (a few microseconds of a call); layouts as Pages, Heads,
+# PagedAttn, PageExps and PagedBatch above.
 _PAGES = struct.Struct("@PP3q3qPq7i0q")
 _HEADS = struct.Struct("@Pqq")
 _PAGED_ATTN = struct.Struct("@qiifI0q")
+_PAGE_EXPS = struct.Struct("@PPqqqq")
+_PAGED_BATCH = struct.Struct("@qqiiii")
 
 
 def _paged_types():
@@ -601,14 +632,17 @@ def _dense(t, name, dtype, like, n) -> int:
     raise ValueError(f"{name} must be a dense tensor of {n} elements")
 
 
-def _pages(k_pages, v_pages, table) -> bytes:
+def _pages(k_pages, v_pages, table, eight=False) -> bytes:
     """gsrq_pages of two pools [pages, page_size, Hkv, head_dim] and their table."""
     torch = _torch()
     shape, dtype, index = k_pages.shape, k_pages.dtype, k_pages.get_device()
     if len(shape) != 4 or v_pages.shape != shape:
         raise ValueError("k_pages and v_pages must be [pages, page_size, Hkv, head_dim], both alike")
-    if dtype is not torch.float16 and dtype is not torch.bfloat16 or v_pages.dtype is not dtype:
-        raise TypeError("pages must be float16 or bfloat16, both alike")
+    if eight:
+        if dtype is not torch.float8_e4m3fn or v_pages.dtype is not dtype:
+            raise TypeError("pages with exponents must be float8_e4m3fn")
+    elif dtype is not torch.float16 and dtype is not torch.bfloat16 or v_pages.dtype is not dtype:
+        raise TypeError("pages must be float16 or bfloat16, both alike (float8_e4m3fn with exponents)")
     if table.dim() != 2 or table.dtype is not torch.int32:
         raise TypeError("table must be a 2-D int32 tensor")
     if v_pages.get_device() != index or table.get_device() != index:
@@ -623,9 +657,28 @@ def _pages(k_pages, v_pages, table) -> bytes:
     try:
         return _PAGES.pack(k_pages.data_ptr(), v_pages.data_ptr(), k0, k1, k2, v0, v1, v2,
                            table.data_ptr(), t0 if B > 1 else per, n, size, per, B, Hkv, hd,
-                           GSRQ_F16 if dtype is torch.float16 else GSRQ_BF16)
+                           GSRQ_E4M3 if eight else GSRQ_F16 if dtype is torch.float16
+                           else GSRQ_BF16)
     except struct.error:
         raise ValueError("a dimension of the pages or the table does not fit 32 bits") from None
+
+
+def _exps(k_exp, v_exp, k_pages):
+    """gsrq_page_exps of two tensors [pages, Hkv] of exponents; None without them."""
+    if k_exp is None and v_exp is None:
+        return None
+    torch = _torch()
+    if k_exp is None or v_exp is None:
+        raise ValueError("k_exp and v_exp come together")
+    shape = (k_pages.shape[0], k_pages.shape[2]) if k_pages.dim() == 4 else ()
+    for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
+        if t.dtype is not torch.int8:
+            raise TypeError(f"{name} must be int8, not {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} must be [pages, Hkv] of the pages, not {tuple(t.shape)}")
+        if t.get_device() != k_pages.get_device():
+            raise ValueError(f"{name} is on {t.device}, expected {k_pages.device}")
+    return _PAGE_EXPS.pack(k_exp.data_ptr(), v_exp.data_ptr(), *k_exp.stride(), *v_exp.stride())
 
 
 def _heads(x, name, heads, head_dim, rows, dtype, like) -> bytes:
@@ -651,8 +704,10 @@ def _empty(like, shape, dtype):
 
 
 def paged_append(k, v, k_pages, v_pages, table, q_start, seq_len, *, q=None, theta=None,
-                 k_norm=None, q_norm=None, eps=1e-6, q_out=None, stream=None):
-    """Put new tokens' keys and values into their pages (see gsrq_paged_append).
+                 k_norm=None, q_norm=None, eps=1e-6, q_out=None, k_exp=None, v_exp=None,
+                 stream=None):
+    """Put new tokens' keys and values into their pages (see gsrq_paged_append,
+    and gsrq_paged_append8 for 8-bit pages).
 
     k, v [T, Hkv, head_dim] and q [T, Hq, head_dim] (float32, float16 or
     bfloat16, any strides); k_pages, v_pages [pages, page_size, Hkv, head_dim]
@@ -664,14 +719,23 @@ def paged_append(k, v, k_pages, v_pages, table, q_start, seq_len, *, q=None, the
     tensor in which rows of no sequence hold anything), or None without q.
     Keys that are also coded (encode, float16 or float32 rows) are coded after
     their norm, which the caller applies for it, and before the rotation:
-    paged_restore turns them and norms nothing."""
+    paged_restore turns them and norms nothing.
+    8-bit pages: k_pages, v_pages float8_e4m3fn with the exponents of their
+    scales, k_exp, v_exp [pages, Hkv] int8 (any strides), which the call updates;
+    the queries come in q_out's type, or else q's, of float32 rows bfloat16."""
     torch = _torch()
     lib = _lib or load_library()
-    pages = _pages(k_pages, v_pages, table)
+    exps = _exps(k_exp, v_exp, k_pages)
+    pages = _pages(k_pages, v_pages, table, exps is not None)
     B = table.shape[0]
     _, _, Hkv, hd = k_pages.shape
     T, dtype, held = k.shape[0], k.dtype, k_pages.dtype
     dt = _paged_dtype(k, "k")
+    if exps is not None:
+        held = (q_out.dtype if q_out is not None else
+                torch.bfloat16 if dtype is torch.float32 else dtype)
+        if held is not torch.float16 and held is not torch.bfloat16:
+            raise TypeError(f"q_out must be float16 or bfloat16, not {held}")
     kh = _heads(k, "k", Hkv, hd, T, dtype, k_pages)
     vh = _heads(v, "v", Hkv, hd, T, dtype, k_pages)
     Hq, qh = 0, None
@@ -692,7 +756,14 @@ def paged_append(k, v, k_pages, v_pages, table, q_start, seq_len, *, q=None, the
         out = q_out
         if q is not None and out is None:
             out = _empty(q, (T, Hq, hd), held)
-        if T > 0:
+        if T > 0 and exps is not None:
+            st = lib.gsrq_paged_append8(pages, exps, T, start, lens, kh, vh, qh, Hq, dt, angles,
+                                        kn, qn, eps, _ptr(out),
+                                        GSRQ_F16 if held is torch.float16 else GSRQ_BF16,
+                                        _append_stream_handle(stream))
+            if st != GSRQ_OK:
+                _check(st, "gsrq_paged_append8")
+        elif T > 0:
             st = lib.gsrq_paged_append(pages, T, start, lens, kh, vh, qh, Hq, dt, angles, kn, qn,
                                        eps, _ptr(out), _append_stream_handle(stream))
             if st != GSRQ_OK:
@@ -707,30 +778,38 @@ def paged_append(k, v, k_pages, v_pages, table, q_start, seq_len, *, q=None, the
 
 
 def attn_paged_workspace_bytes(T, Hq, k_pages, v_pages, table, *, window=0) -> int:
-    """Workspace of attn_paged for T rows of Hq query heads over these pages."""
+    """Workspace of attn_paged for T rows of Hq query heads over these pages, of
+    16 or 8 bits."""
     n = ctypes.c_size_t()
-    _check(load_library().gsrq_attn_paged_workspace_bytes(
-        _PAGED_ATTN.pack(int(T), int(Hq), int(window), 1.0, 0), _pages(k_pages, v_pages, table),
-        ctypes.byref(n)), "gsrq_attn_paged_workspace_bytes")
+    lib, eight = load_library(), k_pages.dtype is _torch().float8_e4m3fn
+    call = lib.gsrq_attn_paged8_workspace_bytes if eight else lib.gsrq_attn_paged_workspace_bytes
+    _check(call(_PAGED_ATTN.pack(int(T), int(Hq), int(window), 1.0, 0),
+                _pages(k_pages, v_pages, table, eight), ctypes.byref(n)),
+           "gsrq_attn_paged_workspace_bytes")
     return int(n.value)
 
 
 def attn_paged(q, k_pages, v_pages, table, q_start, seq_len, *, scale=None, window=0, lse=False,
-               out=None, workspace=None, stream=None):
+               out=None, workspace=None, k_exp=None, v_exp=None, stream=None):
     """Causal attention of new tokens over their sequences' pages (see
     gsrq_attn_paged), after paged_append of the same rows.  q [T, Hq, head_dim]
     of the pages' type, any strides.  Returns out [T, Hq, head_dim] of the
     same type (apart from q; rows of no sequence are left as they are, in a
     new tensor anything), with lse=True also the rows' log-sum-exp [T, Hq]
     float32.  workspace: a uint8 tensor of attn_paged_workspace_bytes, or None (one is
-    made for the call)."""
+    made for the call).  8-bit pages (gsrq_attn_paged8): float8_e4m3fn with
+    k_exp, v_exp [pages, Hkv] int8 as paged_append keeps them, q float16 or
+    bfloat16."""
     torch = _torch()
     lib = _lib or load_library()
-    pages = _pages(k_pages, v_pages, table)
+    exps = _exps(k_exp, v_exp, k_pages)
+    pages = _pages(k_pages, v_pages, table, exps is not None)
     if q.dim() != 3:
         raise ValueError("q must be [T, Hq, head_dim]")
     T, Hq, hd = q.shape
-    B, dtype = table.shape[0], k_pages.dtype
+    B, dtype = table.shape[0], k_pages.dtype if exps is None else q.dtype
+    if exps is not None and dtype is not torch.float16 and dtype is not torch.bfloat16:
+        raise TypeError(f"q must be float16 or bfloat16, not {dtype}")
     qh = _heads(q, "q", Hq, k_pages.shape[3], T, dtype, k_pages)
     start = _dense(q_start, "q_start", torch.int32, k_pages, B + 1)
     lens = _dense(seq_len, "seq_len", torch.int32, k_pages, B)
@@ -749,17 +828,24 @@ def attn_paged(q, k_pages, v_pages, table, q_start, seq_len, *, scale=None, wind
         total = (torch.empty((T, Hq), dtype=torch.float32, device=q.device) if lse else None)
         if T > 0:
             n = ctypes.c_size_t()
-            st = lib.gsrq_attn_paged_workspace_bytes(s, pages, ctypes.byref(n))
+            st = (lib.gsrq_attn_paged_workspace_bytes(s, pages, ctypes.byref(n)) if exps is None
+                  else lib.gsrq_attn_paged8_workspace_bytes(s, pages, ctypes.byref(n)))
             if st != GSRQ_OK:
                 _check(st, "gsrq_attn_paged_workspace_bytes")
             ws, size = None, n.value
             if size:
                 ws = _workspace(size, q.device, workspace)
                 size = ws.numel() * ws.element_size()
-            st = lib.gsrq_attn_paged(s, pages, start, lens, qh, res.data_ptr(), _ptr(total),
-                                     _ptr(ws), size, _append_stream_handle(stream))
+            if exps is None:
+                st = lib.gsrq_attn_paged(s, pages, start, lens, qh, res.data_ptr(), _ptr(total),
+                                         _ptr(ws), size, _append_stream_handle(stream))
+            else:
+                st = lib.gsrq_attn_paged8(s, pages, exps, start, lens, qh,
+                                          GSRQ_F16 if dtype is torch.float16 else GSRQ_BF16,
+                                          res.data_ptr(), _ptr(total), _ptr(ws), size,
+                                          _append_stream_handle(stream))
             if st != GSRQ_OK:
-                _check(st, "gsrq_attn_paged")
+                _check(st, "gsrq_attn_paged" if exps is None else "gsrq_attn_paged8")
         return (res, total) if lse else res
 
     context = _paged_device(k_pages.device, stream)
@@ -812,3 +898,132 @@ def paged_restore(k_codes, v_codes, seq_len, k_gain, k_shape, v_gain, v_shape, k
         return call()
     with context:
         call()
+
+
+def paged_plan(table, free_pages, n_free, seq_len, change, *, page_size, rows, q_start=None,
+               slots=None, positions=None, stream=None):
+    """Pages, rows and slots of a batch whose requests' lengths change (see
+    gsrq_paged_plan): change [B] int32 counts the tokens that every sequence
+    brings or, below zero, gives back.  In place: table [B, per] int32,
+    free_pages [F] int32 with its count n_free [1] int32, seq_len [B] int32.
+    Returns (q_start [B + 1] int32, slots [rows] int64, positions [rows] int32),
+    new tensors or those given; q_start and seq_len are as paged_append and
+    attn_paged take them.  A sequence that grows but has no rows in q_start was
+    not served: the list, the rows or its table row did not suffice."""
+    torch = _torch()
+    lib = _lib or load_library()
+    if table.dim() != 2 or table.dtype is not torch.int32:
+        raise TypeError("table must be a 2-D int32 tensor")
+    B, per = table.shape
+    t0, t1 = table.stride()
+    if t1 != 1 and per > 1:
+        raise ValueError("entries of a table row must be adjacent")
+    rows = int(rows)
+    if rows < 0:
+        raise ValueError("rows must not be negative")
+    F = free_pages.numel()
+    pool = _dense(free_pages, "free_pages", torch.int32, table, F)
+    count = _dense(n_free, "n_free", torch.int32, table, 1)
+    lens = _dense(seq_len, "seq_len", torch.int32, table, B)
+    moves = _dense(change, "change", torch.int32, table, B)
+    for name, t, dtype, n in (("q_start", q_start, torch.int32, B + 1),
+                              ("slots", slots, torch.int64, rows),
+                              ("positions", positions, torch.int32, rows)):
+        if t is not None:
+            _dense(t, name, dtype, table, n)
+    try:
+        s = _PAGED_BATCH.pack(rows, t0 if B > 1 else per, B, per, page_size, F)
+    except struct.error:
+        raise ValueError("a size does not fit 32 bits, or page_size is no number of tokens") from None
+
+    def call():
+        dev = table.device
+        out = (torch.empty(B + 1, dtype=torch.int32, device=dev) if q_start is None else q_start,
+               torch.empty(rows, dtype=torch.int64, device=dev) if slots is None else slots,
+               torch.empty(rows, dtype=torch.int32, device=dev) if positions is None else positions)
+        st = lib.gsrq_paged_plan(s, table.data_ptr(), pool, count, lens, moves, out[0].data_ptr(),
+                                 out[1].data_ptr() or None, out[2].data_ptr() or None,
+                                 _append_stream_handle(stream))
+        if st != GSRQ_OK:
+            _check(st, "gsrq_paged_plan")
+        return out
+
+    context = _paged_device(table.device, stream)
+    if context is None:
+        return call()
+    with context:
+        return call()
+
+
+def verify_drafts_workspace_bytes(T, V, B) -> int:
+    """Workspace of verify_drafts for T rows of V probabilities, B sequences."""
+    n = ctypes.c_size_t()
+    _check(load_library().gsrq_verify_drafts_workspace_bytes(int(T), int(V), int(B),
+                                                             ctypes.byref(n)),
+           "gsrq_verify_drafts_workspace_bytes")
+    return int(n.value)
+
+
+def verify_drafts(tokens, target, draft, uniform, draw, q_start, *, accepted=None, next_token=None,
+                  workspace=None, stream=None):
+    """How many of every sequence's drafts stand, and the token after them (see
+    gsrq_verify_drafts).  Rows as attn_paged takes them: a sequence's last token
+    and its drafts, tokens [T] int32; target [T, V] and draft [T, V] (or None:
+    drafts chosen without chance) probabilities of the token that follows each
+    row, float32, float16 or bfloat16, rows at any stride; uniform [T] and
+    draw [B] float32 numbers of [0, 1); q_start [B + 1] int32.  Returns
+    (accepted [B], next token [B]) int32, new tensors or those given.  With n
+    rows of a sequence, paged_plan takes its n - 1 - accepted other drafts back."""
+    torch = _torch()
+    lib = _lib or load_library()
+    if target.dim() != 2:
+        raise ValueError("target must be [T, V]")
+    T, V = target.shape
+    B = q_start.numel() - 1
+    if B < 1:
+        raise ValueError("q_start must be [B + 1], of one sequence or more")
+    dt, ld = _paged_dtype(target, "target"), [V, V]
+    for i, (name, t) in enumerate((("target", target), ("draft", draft))):
+        if t is None:
+            continue
+        if t.shape != target.shape or t.dtype is not target.dtype:
+            raise ValueError(f"{name} must be like target")
+        if t.get_device() != target.get_device():
+            raise ValueError(f"{name} is on {t.device}, expected {target.device}")
+        s0, s1 = t.stride()
+        if (s1 != 1 and V > 1) or (T > 1 and s0 < V):
+            raise ValueError(f"{name}: a row's probabilities must be adjacent, rows apart")
+        ld[i] = s0 if T > 1 else V
+    ids = _dense(tokens, "tokens", torch.int32, target, T)
+    u = _dense(uniform, "uniform", torch.float32, target, T)
+    d = _dense(draw, "draw", torch.float32, target, B)
+    start = _dense(q_start, "q_start", torch.int32, target, B + 1)
+    for name, t in (("accepted", accepted), ("next_token", next_token)):
+        if t is not None:
+            _dense(t, name, torch.int32, target, B)
+    if workspace is not None and (workspace.device != target.device
+                                  or not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be contiguous, on {target.device}")
+
+    def call():
+        dev = target.device
+        out = (torch.empty(B, dtype=torch.int32, device=dev) if accepted is None else accepted,
+               torch.empty(B, dtype=torch.int32, device=dev) if next_token is None else next_token)
+        n = ctypes.c_size_t()
+        st = lib.gsrq_verify_drafts_workspace_bytes(T, V, B, ctypes.byref(n))
+        if st != GSRQ_OK:
+            _check(st, "gsrq_verify_drafts_workspace_bytes")
+        ws = _workspace(n.value, dev, workspace)
+        st = lib.gsrq_verify_drafts(T, V, B, ids or None, target.data_ptr() or None, ld[0],
+                                    _ptr(draft), ld[1], dt, u or None, d, start,
+                                    out[0].data_ptr(), out[1].data_ptr(), ws.data_ptr(),
+                                    ws.numel() * ws.element_size(), _append_stream_handle(stream))
+        if st != GSRQ_OK:
+            _check(st, "gsrq_verify_drafts")
+        return out
+
+    context = _paged_device(target.device, stream)
+    if context is None:
+        return call()
+    with context:
+        return call()
