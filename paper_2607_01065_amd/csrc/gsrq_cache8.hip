@@ -83,54 +83,123 @@ __device__ __forceinline__ int64_t page_slot_of(const Append8Args& a, int b) {
   return (int64_t)((q < 0 ? 0 : (q > a.T ? a.T : q)) >> a.pool.shift) + 2 * (int64_t)b;
 }
 
-// A head's 16 elements of one lane, in F, with norm and rotation: 8 of the lower
-// half and the 8 they are turned with.  L lanes share a head, all of them
-// active.
-template <typename F, typename TI, int HD>
-__device__ __forceinline__ void normed(const TI* src, const float* norm, float eps, int l,
-                                       F (&lo)[8], F (&hi)[8]) {
-  float x[8], y[8];
-  load8(src + 8 * l, x);
-  load8(src + HD / 2 + 8 * l, y);
+// A head's 16 elements of one lane: 8 of the lower half and the 8 they are turned
+// with.  As they come (two or four registers for four elements), and as numbers.
+template <typename TI> struct Raw {
+  typedef u4 part[sizeof(TI) == 4 ? 2 : 1];
+  part lo, hi;
+  __device__ __forceinline__ void load(const TI* src, int half) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) { lo[j] = x[j]; hi[j] = y[j]; }
-  if (!norm) return;
+    for (int i = 0; i < (int)(sizeof(part) / 16); ++i) {
+      lo[i] = ((const u4*)src)[i];
+      hi[i] = ((const u4*)(src + half))[i];
+    }
+  }
+  __device__ __forceinline__ void get(float (&x)[8], float (&y)[8]) const {
+    load8((const TI*)&lo, x);
+    load8((const TI*)&hi, y);
+  }
+};
+
+// 1 / sqrt(mean square + eps) of a head, in F; its L lanes all active.
+template <typename F, int HD>
+__device__ __forceinline__ F norm_factor(const float (&lo)[8], const float (&hi)[8], float eps) {
   F ss = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) ss = fma(lo[j], lo[j], fma(hi[j], hi[j], ss));
+  for (int j = 0; j < 8; ++j) ss = fma((F)lo[j], (F)lo[j], fma((F)hi[j], (F)hi[j], ss));
 #pragma unroll
   for (int m = 1; m < HD / 16; m <<= 1) ss += __shfl_xor(ss, m);
-  const F r = (F)1 / sqrt(ss * ((F)1 / HD) + (F)eps);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    lo[j] *= r * (F)norm[8 * l + j];
-    hi[j] *= r * (F)norm[HD / 2 + 8 * l + j];
-  }
+  return (F)1 / sqrt(ss * ((F)1 / HD) + (F)eps);
 }
 
-template <typename F>
-__device__ __forceinline__ void turned(F (&lo)[8], F (&hi)[8], int j, F c, F s) {
-  const F x = lo[j], y = hi[j];
-  lo[j] = x * c - y * s;
-  hi[j] = y * c + x * s;
+template <typename F> __device__ __forceinline__ void turned(F& lo, F& hi, F c, F s) {
+  const F x = lo, y = hi;
+  lo = x * c - y * s;
+  hi = y * c + x * s;
 }
+
+// The turns of a lane's 8 pairs at a position.
+struct Turns {
+  float c[8], s[8];
+  __device__ __forceinline__ void at(int64_t pos, const double* theta) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      turn_of(pos, theta[j], c[j], s[j]);
+      __builtin_amdgcn_sched_barrier(0);             // (one after another: in few registers)
+    }
+  }
+};
 
 __device__ __forceinline__ float finite_size(float x) { return is_finite(x) ? fabsf(x) : 0.f; }
 
+// What an append workgroup of a page works on.
+template <typename TI> struct PageRows {
+  const TI* src;                  // the first new token's first head
+  uint8_t* dst;                   // its page's first place there
+  int64_t st0, st1, ps1, ps2;     // rows: token, head; places: token, head
+  const double* theta;            // or null
+  const float* norm;              // or null
+  int64_t pos;                    // of the first new token
+  float eps;
+  int tokens, heads, kept;        // new tokens, heads, tokens of the page before them
+};
+
+// The largest size of the page's elements by heads, in 64 bits; for a whole
+// workgroup, which has set top64 to zeros.  (Rare: one pair of elements at a
+// time, so that it asks for few registers.)
+template <typename TI, int HD>
+__device__ __forceinline__ void exact_sizes(const PageRows<TI>& w, unsigned long long* top64) {
+  constexpr int L = HD / 16;
+  const int l = threadIdx.x % L;
+  for (int i = threadIdx.x / L; i < w.tokens * w.heads; i += E8_THREADS / L) {
+    const int h = i % w.heads, t = i / w.heads;
+    const TI* src = w.src + t * w.st0 + h * w.st1;
+    double r = 1.0, m = 0.0;
+    if (w.norm) {
+      Raw<TI> x;
+      float lo[8], hi[8];
+      x.load(src + 8 * l, HD / 2);
+      x.get(lo, hi);
+      r = norm_factor<double, HD>(lo, hi, w.eps);
+    }
+#pragma unroll 1
+    for (int j = 8 * l; j < 8 * l + 8; ++j) {
+      double x = (double)(float)src[j], y = (double)(float)src[j + HD / 2];
+      if (w.norm) {
+        x *= r * (double)w.norm[j];
+        y *= r * (double)w.norm[j + HD / 2];
+      }
+      if (w.theta) {
+        double a = (double)(w.pos + t) * (w.theta[j] * 0.15915494309189533577), s, c;
+        a -= rint(a);
+        sincospi(2.0 * a, &s, &c);
+        turned(x, y, c, s);
+      }
+      if (is_finite((float)x)) m = fmax(m, fabs(x));
+      if (is_finite((float)y)) m = fmax(m, fabs(y));
+    }
+    atomicMax(&top64[h], (unsigned long long)__double_as_longlong(m));
+  }
+}
+
+// Items of a page workgroup: a row (token and head) for L lanes, E8_KEEP of them
+// a thread at most where they are kept in registers from the search for the
+// largest size to the rounding; a thread's items share their token as far as
+// they can, so that its 8 sines and cosines serve several heads.
+constexpr int E8_KEEP = 4;
+
 template <typename TI, int HD>
 __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
-  constexpr int L = HD / 16, RP = E8_THREADS / L, TG = 32;    // rows at once, tokens of one table
-  __shared__ float2 turns[TG][HD / 2];
+  constexpr int L = HD / 16, RP = E8_THREADS / L;             // lanes of a row, rows at once
   __shared__ uint32_t top[E8_THREADS];                        // bits of the largest sizes, by head
   __shared__ unsigned long long top64[E8_THREADS];
   __shared__ int was[E8_THREADS], now[E8_THREADS];
   __shared__ int close, risen;
-  const int tid = threadIdx.x, lane = tid & 63, l = tid % L;
+  const int tid = threadIdx.x, lane = tid & 63, l = tid % L, row = tid / L;
   const int sub = (int)(wg % (2 * a.groups));
   const int64_t slot = wg / (2 * a.groups);
   const bool key = sub < a.groups;
   const int h0 = (key ? sub : sub - a.groups) * a.HG;
-  const int heads = min(a.HG, a.pool.Hkv - h0);
   int b = 0;
   for (int i = 0; i < a.pool.B; i += 64) {
     const bool done = i + lane < a.pool.B && page_slot_of(a, i + lane + 1) <= slot;
@@ -148,108 +217,157 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
   if (begin >= end) return;
   const int page = page_of(a.pool, b, begin);
   if (page < 0) return;
-  const int kept = (int)(begin & ((1 << a.pool.shift) - 1));  // tokens of the page before the new ones
-  const int tokens = (int)(end - begin), row0 = first + (int)(begin - pos0);
   const int64_t* st = key ? a.kst : a.vst;
   const int64_t* ps = key ? a.pool.ks : a.pool.vs;
-  const TI* src = (const TI*)(key ? a.k : a.v) + row0 * st[0] + h0 * st[1];
-  uint8_t* dst = (uint8_t*)(key ? a.pool.k : a.pool.v) + page * ps[0] + h0 * ps[2];
-  int8_t* exps = key ? a.exps.k + page * a.exps.ks[0] + h0 * a.exps.ks[1]
-                     : a.exps.v + page * a.exps.vs[0] + h0 * a.exps.vs[1];
-  const int64_t es = key ? a.exps.ks[1] : a.exps.vs[1];
-  const float* norm = key ? a.k_norm : nullptr;
-  const bool turn = key && a.theta;
+  const int64_t* es = key ? a.exps.ks : a.exps.vs;
+  PageRows<TI> w;
+  w.src = (const TI*)(key ? a.k : a.v) + (first + (begin - pos0)) * st[0] + h0 * st[1];
+  w.dst = (uint8_t*)(key ? a.pool.k : a.pool.v) + page * ps[0] + h0 * ps[2];
+  w.st0 = st[0]; w.st1 = st[1]; w.ps1 = ps[1]; w.ps2 = ps[2];
+  w.theta = key ? a.theta : nullptr;
+  w.norm = key ? a.k_norm : nullptr;
+  w.pos = begin;
+  w.eps = a.eps;
+  w.tokens = (int)(end - begin);
+  w.heads = min(a.HG, a.pool.Hkv - h0);
+  w.kept = (int)(begin & ((1 << a.pool.shift) - 1));
+  int8_t* exps = (key ? a.exps.k : a.exps.v) + page * es[0] + h0 * es[1];
 
-  // f(item's head, token, its 16 elements) for all items of the page; items are
-  // whole for their L lanes
-  auto each = [&](auto f) __attribute__((always_inline)) {
-    for (int t0 = 0; t0 < tokens; t0 += TG) {
-      const int nt = min(TG, tokens - t0);
-      if (turn) {
-        __syncthreads();
-        for (int i = tid; i < nt * (HD / 2); i += E8_THREADS) {
-          float2 x;
-          turn_of(begin + t0 + i / (HD / 2), a.theta[i % (HD / 2)], x.x, x.y);
-          turns[i / (HD / 2)][i % (HD / 2)] = x;
-        }
-        __syncthreads();
-      }
-      for (int i = tid / L; i < nt * heads; i += RP) {
-        const int h = i % heads, t = i / heads;
-        float lo[8], hi[8];
-        normed<float, TI, HD>(src + (t0 + t) * st[0] + h * st[1], norm, a.eps, l, lo, hi);
-        if (turn) {
+  // item i of this thread; whether there is one (whole for its L lanes)
+  const bool wide = w.tokens <= RP;
+  const int beside = wide ? RP / w.tokens : 1;                // heads side by side
+  const int token0 = wide ? row % w.tokens : row, head0 = wide ? row / w.tokens : 0;
+  const int items = wide ? (w.heads + beside - 1) / beside : w.heads * ((w.tokens + RP - 1) / RP);
+  auto item = [&](int i, int& t, int& h) __attribute__((always_inline)) {
+    t = wide ? token0 : token0 + RP * (i / w.heads);
+    h = wide ? head0 + i * beside : i % w.heads;
+    return i < items && t < w.tokens && h < w.heads && (!wide || head0 < beside);
+  };
+  auto numbers_of = [&](const Raw<TI>& x, int t, int& turned_to, Turns& turns, float (&lo)[8],
+                        float (&hi)[8]) __attribute__((always_inline)) {
+    x.get(lo, hi);
+    if (w.norm) {
+      const float r = norm_factor<float, HD>(lo, hi, w.eps);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float2 x = turns[t][8 * l + j];
-            turned(lo, hi, j, x.x, x.y);
-          }
-        }
-        f(h, t0 + t, lo, hi);
+      for (int j = 0; j < 8; ++j) {
+        lo[j] *= r * w.norm[8 * l + j];
+        hi[j] *= r * w.norm[HD / 2 + 8 * l + j];
       }
     }
+    if (w.theta) {
+      if (t != turned_to) turns.at(w.pos + t, w.theta + 8 * l);
+      turned_to = t;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) turned(lo[j], hi[j], turns.c[j], turns.s[j]);
+    }
   };
-
-  for (int h = tid; h < heads; h += E8_THREADS) {
-    top[h] = 0;
-    top64[h] = 0;
-  }
-  if (tid == 0) close = risen = 0;
-  __syncthreads();
-  each([&](int h, int, const float (&lo)[8], const float (&hi)[8]) __attribute__((always_inline)) {
+  auto search = [&](int h, const float (&lo)[8], const float (&hi)[8]) __attribute__((always_inline)) {
     float m = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) m = fmaxf(m, fmaxf(finite_size(lo[j]), finite_size(hi[j])));
 #pragma unroll
     for (int x = 1; x < L; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
     if (l == 0) atomicMax(&top[h], __float_as_uint(m));
-  });
+  };
+  auto round = [&](int t, int h, const float (&lo)[8], const float (&hi)[8])
+                   __attribute__((always_inline)) {
+    const float f = pow2(-now[h]);
+    uint8_t* to = w.dst + (w.kept + t) * w.ps1 + h * w.ps2 + 8 * l;
+    uint2 x, y;
+    x.x = codes4(lo[0] * f, lo[1] * f, lo[2] * f, lo[3] * f);
+    x.y = codes4(lo[4] * f, lo[5] * f, lo[6] * f, lo[7] * f);
+    y.x = codes4(hi[0] * f, hi[1] * f, hi[2] * f, hi[3] * f);
+    y.y = codes4(hi[4] * f, hi[5] * f, hi[6] * f, hi[7] * f);
+    *(uint2*)to = x;
+    *(uint2*)(to + HD / 2) = y;
+  };
+
+  Raw<TI> kept[E8_KEEP];
+  const bool keep = items <= E8_KEEP;
+  if (keep) {
+#pragma unroll
+    for (int i = 0; i < E8_KEEP; ++i) {
+      int t, h;
+      if (item(i, t, h)) kept[i].load(w.src + t * w.st0 + h * w.st1 + 8 * l, HD / 2);
+    }
+  }
+  for (int h = tid; h < w.heads; h += E8_THREADS) {
+    top[h] = 0;
+    top64[h] = 0;
+    was[h] = held_exp(exps[h * es[1]]);
+  }
+  if (tid == 0) close = risen = 0;
+  __syncthreads();
+  Turns turns;
+  int turned_to = -1;
+  float lo[8], hi[8];
+  if (keep) {
+#pragma unroll
+    for (int i = 0; i < E8_KEEP; ++i) {
+      int t, h;
+      if (item(i, t, h)) {
+        numbers_of(kept[i], t, turned_to, turns, lo, hi);
+        search(h, lo, hi);
+      }
+    }
+  } else {
+    for (int i = 0; i < items; ++i) {
+      int t, h;
+      if (!item(i, t, h)) continue;
+      Raw<TI> x;
+      x.load(w.src + t * w.st0 + h * w.st1 + 8 * l, HD / 2);
+      numbers_of(x, t, turned_to, turns, lo, hi);
+      search(h, lo, hi);
+    }
+  }
   __syncthreads();
   // An exponent that the roundings of norm and rotation (2^-21 of a, at the most)
   // could change is taken from 64-bit numbers.
-  for (int h = tid; h < heads; h += E8_THREADS) {
+  for (int h = tid; h < w.heads; h += E8_THREADS) {
     const float m = __uint_as_float(top[h]);
-    if ((norm || turn) && exp_for(m * (1.f - 0x1p-18f)) != exp_for(m * (1.f + 0x1p-18f))) close = 1;
     now[h] = exp_for(m);
+    if ((w.norm || w.theta) && exp_for(m * (1.f - 0x1p-18f)) != exp_for(m * (1.f + 0x1p-18f)))
+      close = 1;
   }
   __syncthreads();
   if (close) {
-    for (int i = tid / L; i < tokens * heads; i += RP) {
-      const int h = i % heads, t = i / heads;
-      double lo[8], hi[8], m = 0.0;
-      normed<double, TI, HD>(src + t * st[0] + h * st[1], norm, a.eps, l, lo, hi);
-      for (int j = 0; j < 8; ++j) {
-        if (turn) {
-          double r = (double)(begin + t) * (a.theta[8 * l + j] * 0.15915494309189533577), s, c;
-          r -= rint(r);
-          sincospi(2.0 * r, &s, &c);
-          turned(lo, hi, j, c, s);
-        }
-        if (is_finite((float)lo[j])) m = fmax(m, fabs(lo[j]));
-        if (is_finite((float)hi[j])) m = fmax(m, fabs(hi[j]));
-      }
-      atomicMax(&top64[h], (unsigned long long)__double_as_longlong(m));
-    }
-    __syncthreads();
-    for (int h = tid; h < heads; h += E8_THREADS)
-      now[h] = exp_for(__longlong_as_double((long long)top64[h]));
+    exact_sizes<TI, HD>(w, top64);
     __syncthreads();
   }
-  for (int h = tid; h < heads; h += E8_THREADS) {
-    const int before = held_exp(exps[h * es]);
-    was[h] = before;
-    if (kept) now[h] = max(now[h], before);
-    if (kept && now[h] > before) risen = 1;
-    exps[h * es] = (int8_t)now[h];
+  for (int h = tid; h < w.heads; h += E8_THREADS) {
+    int e = close ? exp_for(__longlong_as_double((long long)top64[h])) : now[h];
+    if (w.kept && was[h] > e) e = was[h];
+    if (w.kept && e > was[h]) risen = 1;
+    now[h] = e;
+    exps[h * es[1]] = (int8_t)e;
   }
   __syncthreads();
-  if (risen) {
-    const int n16 = HD / 16;
-    for (int i = tid; i < kept * heads * n16; i += E8_THREADS) {
-      const int c = i % n16, h = i / n16 % heads, t = i / n16 / heads;
+  if (keep) {
+#pragma unroll
+    for (int i = 0; i < E8_KEEP; ++i) {
+      int t, h;
+      if (item(i, t, h)) {
+        numbers_of(kept[i], t, turned_to, turns, lo, hi);
+        round(t, h, lo, hi);
+      }
+    }
+  } else {
+    for (int i = 0; i < items; ++i) {
+      int t, h;
+      if (!item(i, t, h)) continue;
+      Raw<TI> x;
+      x.load(w.src + t * w.st0 + h * w.st1 + 8 * l, HD / 2);
+      numbers_of(x, t, turned_to, turns, lo, hi);
+      round(t, h, lo, hi);
+    }
+  }
+  if (risen) {                    // the tokens before: their codes under the new scale
+    constexpr int N = HD / 16;
+    for (int i = tid; i < w.kept * w.heads * N; i += E8_THREADS) {
+      const int c = i % N, h = i / N % w.heads, t = i / N / w.heads;
       if (now[h] == was[h]) continue;
       const float f = pow2(was[h] - now[h]);
-      u4* at = (u4*)(dst + t * ps[1] + h * ps[2] + 16 * c);
+      u4* at = (u4*)(w.dst + t * w.ps1 + h * w.ps2 + 16 * c);
       u4 x = *at;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -260,50 +378,69 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
       *at = x;
     }
   }
-  each([&](int h, int t, const float (&lo)[8], const float (&hi)[8]) __attribute__((always_inline)) {
-    const float f = pow2(-now[h]);
-    uint8_t* to = dst + (kept + t) * ps[1] + h * ps[2] + 8 * l;
-    uint2 x, y;
-    x.x = codes4(lo[0] * f, lo[1] * f, lo[2] * f, lo[3] * f);
-    x.y = codes4(lo[4] * f, lo[5] * f, lo[6] * f, lo[7] * f);
-    y.x = codes4(hi[0] * f, hi[1] * f, hi[2] * f, hi[3] * f);
-    y.y = codes4(hi[4] * f, hi[5] * f, hi[6] * f, hi[7] * f);
-    *(uint2*)to = x;
-    *(uint2*)(to + HD / 2) = y;
-  });
 }
 
-// Queries: a token's heads, as paged_append_kernel takes them.
+// Queries: E8_ROWS tokens, a row of lanes per head.  All their loads are on the
+// way while the threads share the sines and cosines out among themselves.
+constexpr int E8_ROWS = 4;
+
 template <typename TI, typename TQ, int HD>
 __device__ __forceinline__ void append_queries(const Append8Args& a, int64_t wg) {
-  constexpr int L = HD / 16, RP = E8_THREADS / L;
+  constexpr int L = HD / 16, RP = E8_THREADS / L, HALF = HD / 2;
+  __shared__ float2 turns[E8_ROWS][HALF];
   const int tid = threadIdx.x, l = tid % L;
   const int per = (a.Hq + RP - 1) / RP;
-  const int row = (int)(wg / per), h = (int)(wg % per) * RP + tid / L;
-  const int b = sequence_of(a.q_start, a.pool.B, row);
-  if (b < 0) return;
-  int first, n;
-  new_rows(a.q_start, b, a.T, first, n);
-  const int64_t pos = (int64_t)a.seq_len[b] - n + (row - first);
-  __shared__ float2 turns[HD / 2];
-  if (a.theta) {
-    for (int j = tid; j < HD / 2; j += E8_THREADS) turn_of(pos, a.theta[j], turns[j].x, turns[j].y);
-    __syncthreads();
+  const int row0 = (int)(wg / per) * E8_ROWS, h = (int)(wg % per) * RP + tid / L;
+  const int rows = min(E8_ROWS, a.T - row0);
+  const bool mine = h < a.Hq;
+  Raw<TI> x[E8_ROWS];
+  int64_t pos[E8_ROWS];
+#pragma unroll
+  for (int i = 0; i < E8_ROWS; ++i)
+    if (mine && i < rows)
+      x[i].load((const TI*)a.q + (row0 + i) * a.qst[0] + h * a.qst[1] + 8 * l, HALF);
+#pragma unroll
+  for (int i = 0; i < E8_ROWS; ++i) {
+    pos[i] = INT64_MIN;                                // a row of no sequence
+    const int b = i < rows ? sequence_of(a.q_start, a.pool.B, row0 + i) : -1;
+    if (b < 0) continue;
+    int first, n;
+    new_rows(a.q_start, b, a.T, first, n);
+    pos[i] = (int64_t)a.seq_len[b] - n + (row0 + i - first);
   }
-  if (h >= a.Hq) return;
-  float lo[8], hi[8];
-  normed<float, TI, HD>((const TI*)a.q + row * a.qst[0] + h * a.qst[1], a.q_norm, a.eps, l, lo, hi);
   if (a.theta) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) turned(lo, hi, j, turns[8 * l + j].x, turns[8 * l + j].y);
+    for (int i = 0; i < E8_ROWS; ++i)                  // (HALF divides 256: a thread's pairs are all one)
+      if (i % (E8_THREADS / HALF) == tid / HALF && pos[i] != INT64_MIN)
+        turn_of(pos[i], a.theta[tid % HALF], turns[i][tid % HALF].x, turns[i][tid % HALF].y);
+    __syncthreads();
   }
-  TQ* dst = (TQ*)a.q_out + ((int64_t)row * a.Hq + h) * HD + 8 * l;
-  store8(dst, lo);
-  store8(dst + HD / 2, hi);
+  if (!mine) return;
+#pragma unroll
+  for (int i = 0; i < E8_ROWS; ++i) {
+    if (pos[i] == INT64_MIN) continue;
+    float lo[8], hi[8];
+    x[i].get(lo, hi);
+    if (a.q_norm) {
+      const float r = norm_factor<float, HD>(lo, hi, a.eps);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        lo[j] *= r * a.q_norm[8 * l + j];
+        hi[j] *= r * a.q_norm[HALF + 8 * l + j];
+      }
+    }
+    if (a.theta) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) turned(lo[j], hi[j], turns[i][8 * l + j].x, turns[i][8 * l + j].y);
+    }
+    TQ* dst = (TQ*)a.q_out + ((int64_t)(row0 + i) * a.Hq + h) * HD + 8 * l;
+    store8(dst, lo);
+    store8(dst + HALF, hi);
+  }
 }
 
 template <typename TI, typename TQ, int HD>
-__global__ void __launch_bounds__(E8_THREADS) cache8_append_kernel(Append8Args a) {
+__global__ void __launch_bounds__(E8_THREADS, sizeof(TI) == 4 ? 3 : 4) cache8_append_kernel(Append8Args a) {
   if ((int64_t)blockIdx.x < a.page_wgs) append_page<TI, HD>(a, blockIdx.x);
   else append_queries<TI, TQ, HD>(a, (int64_t)blockIdx.x - a.page_wgs);
 }
@@ -1022,11 +1159,14 @@ gsrq_status gsrq_paged_append8(const gsrq_pages* pages, const gsrq_page_exps* ex
   if (T > MAX_BLOCKS || a.pool.B > (1 << 20)) return GSRQ_E_UNSUPPORTED;
   if (2ll * a.pool.Hkv + (q ? Hq : 0) > 65535) return GSRQ_E_UNSUPPORTED;
   const int hd = pages->head_dim, rows = E8_THREADS * 16 / hd;
-  a.HG = std::min(a.pool.Hkv, std::max(1, 2 * rows / (int)std::min<int64_t>(pages->page_size, T)));
+  // as many heads as E8_KEEP items a thread hold of a page's tokens
+  const int tokens = (int)std::min<int64_t>(pages->page_size, T);
+  const int most = tokens <= rows ? E8_KEEP * (rows / tokens) : E8_KEEP / ((tokens + rows - 1) / rows);
+  a.HG = std::min(a.pool.Hkv, std::max(1, most));
   a.groups = (a.pool.Hkv + a.HG - 1) / a.HG;
   a.page_wgs = ((T >> a.pool.shift) + 2ll * a.pool.B) * 2 * a.groups;
   a.Hq = q ? Hq : 0;
-  const int64_t wgs = a.page_wgs + T * ((a.Hq + rows - 1) / rows);
+  const int64_t wgs = a.page_wgs + (T + E8_ROWS - 1) / E8_ROWS * ((a.Hq + rows - 1) / rows);
   if (wgs > MAX_BLOCKS) return GSRQ_E_UNSUPPORTED;
   a.k = k->data;
   a.v = v->data;

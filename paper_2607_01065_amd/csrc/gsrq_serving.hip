@@ -41,24 +41,30 @@ __device__ __forceinline__ int sum_of(int a, int b) {
   return s > (uint32_t)INT32_MAX ? INT32_MAX : (int)s;
 }
 
-// The sum of the threads' x in front of this one, and of all (in `all`); for the
-// whole workgroup.
-__device__ __forceinline__ int sum_before(int x, int* wave_sums, int& all) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int s = x;
+// The sums of the threads' x in front of this one, and of all (in `all`); for
+// the whole workgroup, of whole waves.
+__device__ __forceinline__ int2 sums_before(int2 x, int2* wave_sums, int2& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  int2 s = x;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(s, d);
-    s = lane >= d ? sum_of(s, y) : s;
+    const int y = __shfl_up(s.x, d), z = __shfl_up(s.y, d);
+    s.x = lane >= d ? sum_of(s.x, y) : s.x;
+    s.y = lane >= d ? sum_of(s.y, z) : s.y;
+  }
+  const int up = __shfl_up(s.x, 1), up2 = __shfl_up(s.y, 1);
+  int2 before = make_int2(lane ? up : 0, lane ? up2 : 0);
+  if (waves == 1) {
+    all = make_int2(__shfl(s.x, 63), __shfl(s.y, 63));
+    return before;
   }
   if (lane == 63) wave_sums[wave] = s;
-  const int up = __shfl_up(s, 1);
-  int before = lane ? up : 0;
   __syncthreads();
-  all = 0;
-  for (int i = 0; i < PL_THREADS / 64; ++i) {
-    if (i < wave) before = sum_of(before, wave_sums[i]);
-    all = sum_of(all, wave_sums[i]);
+  all = make_int2(0, 0);
+  for (int i = 0; i < waves; ++i) {
+    const int2 y = wave_sums[i];
+    if (i < wave) before = make_int2(sum_of(before.x, y.x), sum_of(before.y, y.y));
+    all = make_int2(sum_of(all.x, y.x), sum_of(all.y, y.y));
   }
   __syncthreads();
   return before;
@@ -108,79 +114,76 @@ __device__ __forceinline__ void write_slot(const PlanArgs& a, int row) {
 
 __global__ void __launch_bounds__(PL_THREADS) plan_update_kernel(PlanArgs a, int rows_too) {
   __shared__ int first[PL_MOST + 1], who[PL_MOST];
-  __shared__ int wave_sums[PL_THREADS / 64];
-  const int tid = threadIdx.x;
-  // pages that are given back: how many entries each sequence has of them
-  int base = 0, all;
-  for (int b0 = 0; b0 < a.B; b0 += PL_THREADS) {
-    const int b = b0 + tid;
-    int x = 0;
-    if (b < a.B) {
-      const Ask q = ask_of(a, b);
-      x = max(q.old_pages - q.new_pages, 0);
-    }
-    const int before = sum_before(x, wave_sums, all);
-    if (b < a.B) first[b] = sum_of(base, before);
-    base = sum_of(base, all);
-  }
-  if (tid == 0) first[a.B] = base;
-  __syncthreads();
-  // from the last entry to the first, so that taking as many again brings them
-  // in the order of the sequences; entries without a page are left out
+  __shared__ int2 wave_sums[PL_THREADS / 64];
+  const int tid = threadIdx.x, NT = blockDim.x;
   int count = *a.n_free;
-  count = count < 0 ? 0 : (count > a.F ? a.F : count);
-  for (int i0 = 0; i0 < base; i0 += PL_THREADS) {
-    const int i = base - 1 - i0 - tid;
-    int page = -1;
-    if (i >= 0) {
-      const int b = owner(first, a.B, i);
-      const Ask q = ask_of(a, b);
-      int32_t* entry = a.table + b * a.ldt + q.new_pages + (i - first[b]);
-      page = *entry;
-      *entry = -1;
-    }
-    const int at = sum_before(page >= 0, wave_sums, all);
-    if (page >= 0 && count + (int64_t)at < a.F) a.free[count + at] = page;
-    count = (int)min((int64_t)a.F, (int64_t)count + all);
-  }
-  __syncthreads();                                     // (workgroup: the list is one CU's)
-  // who fits, in order, and what those who fit take
-  int pages = 0, rows = 0, got = 0, out = 0;
-  for (int b0 = 0; b0 < a.B; b0 += PL_THREADS) {
+  // pages that are given back: how many entries each sequence has of them
+  int base = 0;
+  Ask q = {};
+  for (int b0 = 0; b0 < a.B; b0 += NT) {
     const int b = b0 + tid;
-    Ask q = {};
-    int need = 0, more = 0;
-    if (b < a.B) {
-      q = ask_of(a, b);
-      need = max(q.new_pages - q.old_pages, 0);
-      more = q.want < 0 ? 0 : max(q.want - q.had, 0);
+    q = (Ask){};
+    if (b < a.B) q = ask_of(a, b);
+    int2 all;
+    const int2 before = sums_before(make_int2(max(q.old_pages - q.new_pages, 0), 0), wave_sums, all);
+    if (b < a.B) first[b] = sum_of(base, before.x);
+    base = sum_of(base, all.x);
+  }
+  count = count < 0 ? 0 : (count > a.F ? a.F : count);
+  if (base) {
+    if (tid == 0) first[a.B] = base;
+    __syncthreads();
+    // from the last entry to the first, so that taking as many again brings them
+    // in the order of the sequences; entries without a page are left out
+    for (int i0 = 0; i0 < base; i0 += NT) {
+      const int i = base - 1 - i0 - tid;
+      int page = -1;
+      if (i >= 0) {
+        const int b = owner(first, a.B, i);
+        const Ask x = ask_of(a, b);
+        int32_t* entry = a.table + b * a.ldt + x.new_pages + (i - first[b]);
+        page = *entry;
+        *entry = -1;
+      }
+      int2 all;
+      const int at = sums_before(make_int2(page >= 0, 0), wave_sums, all).x;
+      if (page >= 0 && count + (int64_t)at < a.F) a.free[count + at] = page;
+      count = (int)min((int64_t)a.F, (int64_t)count + all.x);
     }
-    int all_pages, all_rows;
-    const int p = sum_of(sum_of(pages, sum_before(need, wave_sums, all_pages)), need);
-    const int r = sum_of(sum_of(rows, sum_before(more, wave_sums, all_rows)), more);
-    pages = sum_of(pages, all_pages);
-    rows = sum_of(rows, all_rows);
-    const bool served = b < a.B && q.want >= 0 && (more == 0 || (p <= count && r <= a.T));
-    need = served ? need : 0;
-    more = served ? more : 0;
-    const int p0 = sum_before(need, wave_sums, all_pages);
-    const int r0 = sum_before(more, wave_sums, all_rows);
+    __syncthreads();
+  }
+  // who fits, in order, and what those who fit take
+  int2 asked = make_int2(0, 0), given = make_int2(0, 0);       // pages, rows
+  for (int b0 = 0; b0 < a.B; b0 += NT) {
+    const int b = b0 + tid;
+    if (a.B > NT) {                                            // (else as above)
+      q = (Ask){};
+      if (b < a.B) q = ask_of(a, b);
+    }
+    int2 x = make_int2(0, 0), all;
+    if (b < a.B && q.want >= 0)
+      x = make_int2(max(q.new_pages - q.old_pages, 0), max(q.want - q.had, 0));
+    const int2 before = sums_before(x, wave_sums, all);
+    const int p = sum_of(sum_of(asked.x, before.x), x.x), r = sum_of(sum_of(asked.y, before.y), x.y);
+    asked = make_int2(sum_of(asked.x, all.x), sum_of(asked.y, all.y));
+    const bool served = b < a.B && q.want >= 0 && (x.y == 0 || (p <= count && r <= a.T));
+    const int2 y = served ? x : make_int2(0, 0);
+    const int2 own = sums_before(y, wave_sums, all);
     if (b < a.B) {
-      first[b] = got + p0;
+      first[b] = given.x + own.x;
       who[b] = q.old_pages;
-      a.q_start[b] = out + r0;
+      a.q_start[b] = given.y + own.y;
       a.seq_len[b] = served ? q.want : q.had;
     }
-    got += all_pages;
-    out += all_rows;
+    given = make_int2(given.x + all.x, given.y + all.y);
   }
   if (tid == 0) {
-    first[a.B] = got;
-    a.q_start[a.B] = out;
-    *a.n_free = count - got;
+    first[a.B] = given.x;
+    a.q_start[a.B] = given.y;
+    *a.n_free = count - given.x;
   }
   __syncthreads();
-  for (int i = tid; i < got; i += PL_THREADS) {
+  for (int i = tid; i < given.x; i += NT) {
     const int b = owner(first, a.B, i);
     int32_t* from = a.free + (count - 1 - i);
     a.table[b * a.ldt + who[b] + (i - first[b])] = *from;
@@ -188,7 +191,7 @@ __global__ void __launch_bounds__(PL_THREADS) plan_update_kernel(PlanArgs a, int
   }
   if (!rows_too) return;
   __syncthreads();
-  for (int row = tid; row < a.T; row += PL_THREADS) write_slot(a, row);
+  for (int row = tid; row < a.T; row += NT) write_slot(a, row);
 }
 
 __global__ void __launch_bounds__(256) plan_slots_finalize_kernel(PlanArgs a) {
@@ -206,6 +209,7 @@ struct VerifyArgs {
   const float *uniform, *draw;
   int32_t *accepted, *next;
   double* sums;                   // [B][2][chunks]: of max(p - q, 0), and of p
+  int4* stops;                    // [B] where each sequence's drafts end
   int64_t ldp, ldq;
   int T, V, B, chunk, chunks;
 };
@@ -273,6 +277,7 @@ __global__ void __launch_bounds__(VD_THREADS) verify_sums_kernel(VerifyArgs a) {
   int first;
   bool rejected;
   const int row = stop_of<T>(a, b, first, rejected);
+  if (c == 0 && tid == 0) a.stops[b] = make_int4(row, rejected, first, 0);
   if (row < 0) return;
   const Weights<T> w(a, row, rejected);
   const int end = min(a.V, (c + 1) * a.chunk);
@@ -297,18 +302,35 @@ __global__ void __launch_bounds__(VD_THREADS) verify_sums_kernel(VerifyArgs a) {
   }
 }
 
-// One workgroup per sequence: the chunk that holds the drawn point, by one
-// thread's running sum; then the token, by the threads' sums of what each has of
-// the chunk and one thread's running sum through its share.
+// One workgroup per sequence: the chunk that holds the drawn point, from the
+// chunks' sums, one a lane; then the token, VD_EACH neighbours a thread: the
+// threads' sums in front of each other, and a running sum through the share of
+// the one that passes the point.  (One thread's running sums through chunks and
+// threads: 24 us for 64 sequences.)
+constexpr int VD_EACH = 16;
+constexpr int VD_SPAN = VD_THREADS * VD_EACH;
+
+// The sum up to and with this lane's, in a wave.
+__device__ __forceinline__ double sum_up_to(double x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const double y = __shfl_up(x, d);
+    x += lane >= d ? y : 0.0;
+  }
+  return x;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(VD_THREADS) verify_finalize_kernel(VerifyArgs a) {
-  __shared__ double shares[VD_THREADS];
-  __shared__ double base, point;
-  __shared__ int at, plain, best;
-  const int b = blockIdx.x, tid = threadIdx.x;
-  int first;
-  bool rejected;
-  const int row = stop_of<T>(a, b, first, rejected);
+  __shared__ double ends[VD_THREADS / 64];
+  __shared__ int hit[VD_THREADS / 64], last[VD_THREADS / 64];
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int4 stop = a.stops[b];       // row, whether a draft was rejected there, first row
+  const bool some = lane < a.chunks;
+  const double* s = a.sums + (int64_t)b * 2 * a.chunks + (some ? lane : 0);
+  double mine = s[0], all = s[a.chunks];
+  const int row = stop.x;
   if (row < 0) {
     if (tid == 0) {
       a.accepted[b] = 0;
@@ -316,75 +338,78 @@ __global__ void __launch_bounds__(VD_THREADS) verify_finalize_kernel(VerifyArgs 
     }
     return;
   }
-  if (tid == 0) {
-    const double* s = a.sums + (int64_t)b * 2 * a.chunks;
-    double total = 0.0;
-    for (int c = 0; c < a.chunks; ++c) total += s[c];
-    plain = !(total > 0.0);
-    if (plain) {
-      s += a.chunks;
-      total = 0.0;
-      for (int c = 0; c < a.chunks; ++c) total += s[c];
-    }
-    point = (double)a.draw[b] * total;
-    // the first chunk that passes the point; without one (a draw of 1 or more)
-    // the last that has any weight
-    double run = 0.0;
-    int found = -1, last = -1;
-    for (int c = 0; c < a.chunks && found < 0; ++c) {
-      if (s[c] > 0.0) {
-        last = c;
-        base = run;
+  mine = some ? mine : 0.0;
+  all = some ? all : 0.0;
+  const bool rejected = stop.y && __any(mine > 0.0);
+  mine = rejected ? mine : all;
+  const double upto = sum_up_to(mine);
+  const double point = (double)a.draw[b] * __shfl(upto, 63);
+  // the first chunk that passes the point; without one (a draw of 1 or more) the
+  // last that has any weight
+  const uint64_t weighty = __ballot(mine > 0.0), past = __ballot(mine > 0.0 && upto > point);
+  int token = -1;
+  if (weighty) {
+    const int c = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(weighty);
+    double run = c ? __shfl(upto, c - 1) : 0.0;
+    const Weights<T> w(a, row, rejected);
+    const int begin = c * a.chunk, end = min(a.V, begin + a.chunk);
+    for (int v0 = begin; v0 < end; v0 += VD_SPAN) {
+      double x[VD_EACH], share = 0.0;
+#pragma unroll
+      for (int i = 0; i < VD_EACH; ++i) {
+        const int v = v0 + tid * VD_EACH + i;
+        double rest = 0.0, full = 0.0;
+        if (v < end) w.get(v, rest, full);
+        x[i] = rejected ? rest : full;
+        share += x[i];
       }
-      run += s[c];
-      if (s[c] > 0.0 && run > point) found = c;
+      const double up = sum_up_to(share), before = __shfl_up(up, 1);
+      if (lane == 63) ends[wave] = up;
+      __syncthreads();
+      double at = run, total = 0.0;
+#pragma unroll
+      for (int i = 0; i < VD_THREADS / 64; ++i) {
+        at += i < wave ? ends[i] : 0.0;
+        total += ends[i];
+      }
+      at += lane ? before : 0.0;
+      // the token that passes the point, and the last of any weight
+      int here = -1, heavy = -1;
+#pragma unroll
+      for (int i = 0; i < VD_EACH; ++i) {
+        at += x[i];
+        if (x[i] > 0.0) {
+          heavy = i;
+          if (here < 0 && at > point) here = i;
+        }
+      }
+      const uint64_t passes = __ballot(here >= 0), holds = __ballot(heavy >= 0);
+      const int p = passes ? __builtin_ctzll(passes) : 0;
+      const int h = holds ? 63 - __builtin_clzll(holds) : 0;
+      const int first_here = (wave * 64 + p) * VD_EACH + __shfl(here, p);
+      const int last_heavy = (wave * 64 + h) * VD_EACH + __shfl(heavy, h);
+      if (lane == 0) {
+        hit[wave] = passes ? v0 + first_here : -1;
+        last[wave] = holds ? v0 + last_heavy : -1;
+      }
+      __syncthreads();
+      int found = -1;
+#pragma unroll
+      for (int i = 0; i < VD_THREADS / 64; ++i) {
+        if (last[i] >= 0) token = last[i];
+        if (found < 0) found = hit[i];
+      }
+      if (found >= 0) {
+        token = found;
+        break;
+      }
+      run += total;
+      __syncthreads();
     }
-    at = found >= 0 ? found : last;
-    best = -1;
-  }
-  __syncthreads();
-  if (at >= 0) {
-    const Weights<T> w(a, row, rejected && !plain);
-    const int begin = at * a.chunk, end = min(a.V, begin + a.chunk);
-    const int each = (end - begin + VD_THREADS - 1) / VD_THREADS;
-    const int from = min(end, begin + tid * each), to = min(end, from + each);
-    double s = 0.0;
-    for (int v = from; v < to; ++v) {
-      double x, y;
-      w.get(v, x, y);
-      s += w.rejected ? x : y;
-    }
-    shares[tid] = s;
-    __syncthreads();
-    double run = base;
-    for (int i = 0; i < tid; ++i) run += shares[i];
-    // the token that passes the point in this thread's share, or the last with
-    // any weight up to here (taken where no thread's passes it)
-    int mine = -1;
-    bool passed = false;
-    for (int v = from; v < to && !passed; ++v) {
-      double x, y;
-      w.get(v, x, y);
-      x = w.rejected ? x : y;
-      run += x;
-      if (x > 0.0) mine = v;
-      passed = x > 0.0 && run > point;
-    }
-    // (the first thread that passes it, or else the last token of all)
-    shares[tid] = passed ? 1.0 : 0.0;
-    __syncthreads();
-    bool before = false, any = false;
-    for (int i = 0; i < VD_THREADS; ++i) {
-      const bool x = shares[i] > 0.0;
-      any = any || x;
-      before = before || (x && i < tid);
-    }
-    if (any ? passed && !before : mine >= 0) atomicMax(&best, mine);
-    __syncthreads();
   }
   if (tid == 0) {
-    a.accepted[b] = row - first;
-    a.next[b] = best;
+    a.accepted[b] = row - stop.z;
+    a.next[b] = token;
   }
 }
 
@@ -395,6 +420,10 @@ void verify_chunks(int64_t V, int& chunk, int& chunks) {
   while (c * 64 < V) c *= 2;
   chunk = (int)c;
   chunks = (int)((V + c - 1) / c);
+}
+
+size_t verify_bytes(int64_t B, int chunks) {
+  return align256((size_t)B * sizeof(int4)) + align256((size_t)B * 2 * chunks * sizeof(double));
 }
 
 gsrq_status verify_shape(int64_t T, int64_t V, int64_t B) {
@@ -444,8 +473,12 @@ gsrq_status gsrq_paged_plan(const gsrq_paged_batch* s, int32_t* table, int32_t* 
   a.T = (int)s->T;
   hipStream_t st = (hipStream_t)stream;
   TimedLaunch tl(GSRQ_KERNEL_SERVING, st);
+  // as many threads as there are sequences, or rows that are written too
   const bool one = s->T <= 2 * PL_THREADS;
-  plan_update_kernel<<<1, PL_THREADS, 0, st>>>(a, one);
+  const int64_t work = std::max<int64_t>(s->B, one ? s->T : s->T / s->page_size);
+  int threads = 64;
+  while (threads < PL_THREADS && threads < work) threads *= 2;
+  plan_update_kernel<<<1, threads, 0, st>>>(a, one);
   gsrq_status e = launch_ok();
   if (e || one) return e;
   plan_slots_finalize_kernel<<<(unsigned)((s->T + 255) / 256), 256, 0, st>>>(a);
@@ -458,7 +491,7 @@ gsrq_status gsrq_verify_drafts_workspace_bytes(int64_t T, int64_t V, int32_t B, 
   if (e) return e;
   int chunk, chunks;
   verify_chunks(V, chunk, chunks);
-  *bytes = align256((size_t)B * 2 * chunks * sizeof(double));
+  *bytes = verify_bytes(B, chunks);
   return GSRQ_OK;
 }
 
@@ -478,7 +511,7 @@ gsrq_status gsrq_verify_drafts(int64_t T, int64_t V, int32_t B, const int32_t* t
     return GSRQ_E_ARG;
   VerifyArgs a;
   verify_chunks(V, a.chunk, a.chunks);
-  if (ws_bytes < align256((size_t)B * 2 * a.chunks * sizeof(double))) return GSRQ_E_WORKSPACE;
+  if (ws_bytes < verify_bytes(B, a.chunks)) return GSRQ_E_WORKSPACE;
   a.tokens = tokens;
   a.q_start = q_start;
   a.target = target;
@@ -487,7 +520,8 @@ gsrq_status gsrq_verify_drafts(int64_t T, int64_t V, int32_t B, const int32_t* t
   a.draw = draw;
   a.accepted = accepted;
   a.next = next;
-  a.sums = (double*)workspace;
+  a.stops = (int4*)workspace;
+  a.sums = (double*)((char*)workspace + align256((size_t)B * sizeof(int4)));
   a.ldp = ldp;
   a.ldq = ldq;
   a.T = (int)T;
