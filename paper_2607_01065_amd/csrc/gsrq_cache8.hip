@@ -502,12 +502,13 @@ template <int HD> __device__ __forceinline__ int value_chunk8(int r, int c) {
 // Scales of a tile's groups of eight keys, the same for the whole wave: the
 // factor of a score (log2), and the values' exponent.
 template <int NB> struct Groups {
-  float ck[4 * NB], ev[4 * NB];
+  float ck[4 * NB], ev[4 * NB], iv[4 * NB];           // iv: 2^-ev
 };
 
 // The same, of one page, for the lane that looks it up.
 struct PageScale {
-  float ck, ev;
+  float ck;
+  int ev;
 };
 __device__ __forceinline__ PageScale page_scale(const Pt8Args& a, int head, int page) {
   int k = 0, v = 0;
@@ -516,10 +517,20 @@ __device__ __forceinline__ PageScale page_scale(const Pt8Args& a, int head, int 
     v = held_exp(a.exps.v[page * a.exps.vs[0] + head * a.exps.vs[1]]);
   }
   // (a factor above zero: -inf times zero would be NaN)
-  return {fmaxf(a.p.c * pow2(k), 1.17549435e-38f), (float)v};
+  return {fmaxf(a.p.c * pow2(k), 1.17549435e-38f), v};
 }
-__device__ __forceinline__ float of_lane(float x, int lane) {
-  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
+// Those of a tile whose first group lane `first` has looked up.
+template <int NB>
+__device__ __forceinline__ Groups<NB> groups_from(const PageScale& x, int first) {
+  Groups<NB> g;
+#pragma unroll
+  for (int j = 0; j < 4 * NB; ++j) {
+    const int ev = __builtin_amdgcn_readlane(x.ev, first + j);
+    g.ck[j] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x.ck), first + j));
+    g.ev[j] = (float)ev;
+    g.iv[j] = pow2(-ev);
+  }
+  return g;
 }
 
 // The largest of four products' sums (as max16).
@@ -599,7 +610,7 @@ template <typename T, int HD> struct Columns8 : Columns<T, HD> {
           x[e] = __builtin_amdgcn_exp2f(fmaf(sc[n][4 * j + e], ck, base));
           p[n][j / 2][4 * (j % 2) + e] = (T)x[e];
         }
-        l = fmaf((x[0] + x[1]) + (x[2] + x[3]), __builtin_amdgcn_exp2f(-ev), l);
+        l = fmaf((x[0] + x[1]) + (x[2] + x[3]), g.iv[4 * n + j], l);
       }
   }
 
@@ -690,12 +701,23 @@ __device__ __forceinline__ const char* row_of_load(const char* base, uint64_t of
   return at + within;
 }
 
-// As load_to_lds(), from an address of the lane's own.
+// The rows of a tile that are not there: by groups of eight (bits of `groups`),
+// and behind the `left` that it has.
+template <int ROWS> __device__ __forceinline__ uint64_t gone_rows(uint32_t groups, int left) {
+  uint64_t held = ((groups & 15u) * 0x00204081u & 0x01010101u) * 0xffu;
+  if (ROWS == 64) held |= (uint64_t)((((groups >> 4) & 15u) * 0x00204081u & 0x01010101u) * 0xffu) << 32;
+  const uint64_t behind = left >= ROWS ? 0ull : left <= 0 ? ~0ull : ~0ull << left;
+  return (~held | behind) & (~0ull >> (64 - ROWS));
+}
+
+// As load_to_lds(), from an address of the lane's own, and past the caches: keys and
+// values of few rows are read once (8 sequences of <= 32768 tokens: 94 us a call,
+// 104 with cached loads; 16 of 60000 5.5 TB/s and 5.1).
 __device__ __forceinline__ void load_lane_to_lds(const char* at, uint32_t to) {
   asm volatile(
       "s_mov_b32 m0, %1\n\t"
       "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %0, off"
+      "global_load_lds_dwordx4 %0, off nt"
       :
       : "v"(at), "s"(to)
       : "memory", "m0");
@@ -719,8 +741,9 @@ template <int HD> struct Pt8Cfg {
 };
 
 // 128 queries of one sequence and key head, 32 a wave, and a piece of the keys.
-// Tiles become numbers on their way to LDS, once for the four waves: a wave that
-// converted what it reads would do it four times.
+// Tiles become numbers on their way to LDS, once for the four waves: where each
+// wave converts what it reads (codes in LDS, half its traffic), vector
+// instructions bound it: 874 us against 838 for 1024 tokens over 40000.
 template <typename T, int HD>
 __device__ __forceinline__ void many8(const Pt8Args& a8, char* lds, int block) {
   typedef Pt8Cfg<HD> C;
@@ -761,18 +784,36 @@ __device__ __forceinline__ void many8(const Pt8Args& a8, char* lds, int block) {
     odd_tiles[1] = -1;
   }
 
-  constexpr int NB = C::TN / 32;
-  const int lrow = lane / C::CH, lch = lane % C::CH, mine = lane & (C::TN - 1);
+  // Pages and scales are looked up for several tiles at once, one group of 8
+  // tokens (which lie in one page) a lane, lane GP (tile mod TILES) + group: a
+  // lookup per tile takes as many instructions as a quarter of its weights (838
+  // us against 748 for 1024 tokens over 40000).
+  constexpr int NB = C::TN / 32, GP = 4 * NB, TILES = 64 / GP;
+  const int lrow = lane / C::CH, lch = lane % C::CH;
   const char* const kbase = a.pool.k + head * a.pool.ks[2];
   const char* const vbase = a.pool.v + head * a.pool.vs[2];
-  auto fetch = [&](bool key, int t0, int page, u4 (&raw)[C::PER]) __attribute__((always_inline)) {
+  uint64_t k_at = 0, v_at = 0, there = 0;              // offsets; lanes whose page is there
+  PageScale scale = {1.f, 0};
+  auto token_of = [&](int i) { return begin + i * C::TN + 8 * lane; };
+  int entry = entry_of(a.pool, b, token_of(0));
+  auto look_up = [&](int i) __attribute__((always_inline)) {
+    const int t = token_of(i), page = t < end ? checked(a.pool, entry) : -1;
+    k_at = token_offset8(a.pool, a.pool.ks, page, t);
+    v_at = token_offset8(a.pool, a.pool.vs, page, t);
+    there = __ballot(page >= 0);
+    scale = page_scale(a8, head, page);
+    if (begin + (i + TILES) * C::TN < end) entry = entry_of(a.pool, b, token_of(i + TILES));
+  };
+  auto gone = [&](int i) {
+    return gone_rows<C::TN>((uint32_t)(there >> (GP * (i % TILES))), end - begin - i * C::TN);
+  };
+  auto fetch = [&](bool key, uint64_t at, int i, u4 (&raw)[C::PER]) __attribute__((always_inline)) {
     const int64_t (&st)[3] = key ? a.pool.ks : a.pool.vs;
-    const uint64_t offset = token_offset8(a.pool, st, page, t0 + mine);
 #pragma unroll
     for (int u = 0; u < C::PER; ++u) {
-      const int row = (u * PT_WAVES + wave) * C::RL;
-      raw[u] = *(const u4*)row_of_load<HD>(key ? kbase : vbase, offset, row, row + 8,
-                                           lrow % 8 * (uint32_t)st[1] + 16 * lch);
+      const int row = (u * PT_WAVES + wave) * C::RL, from = GP * (i % TILES) + row / 8;
+      raw[u] = *(const u4*)row_of_load<HD>(key ? kbase : vbase, at, from, from + 1,
+                                           (row % 8 + lrow % 8) * (uint32_t)st[1] + 16 * lch);
     }
   };
   auto put = [&](bool key, const u4 (&raw)[C::PER], char* at) __attribute__((always_inline)) {
@@ -786,40 +827,25 @@ __device__ __forceinline__ void many8(const Pt8Args& a8, char* lds, int block) {
       *(v8*)(at + c1) = numbers<T>(raw[u][2], raw[u][3]);
     }
   };
-  auto page_at = [&](int t0, int entry) __attribute__((always_inline)) {
-    return t0 + mine < end ? checked(a.pool, entry) : -1;
-  };
-  auto groups_of = [&](const PageScale& x) __attribute__((always_inline)) {
-    Groups<NB> g;
-#pragma unroll
-    for (int j = 0; j < 4 * NB; ++j) {
-      g.ck[j] = of_lane(x.ck, 8 * j);
-      g.ev[j] = of_lane(x.ev, 8 * j);
-    }
-    return g;
-  };
   // Keys run one tile ahead of values, as over 16-bit pages; both are read one
   // tile before they go to LDS.
   char* const kt = lds;
   char* const vt = lds + 2 * C::BYTES;
   u4 rk[C::PER], rv[C::PER];
-  int page = page_at(begin, entry_of(a.pool, b, begin + mine));
-  int next = page_at(begin + C::TN, entry_of(a.pool, b, begin + C::TN + mine));
-  uint64_t absent = __ballot(page < 0), next_absent = __ballot(next < 0);
-  fetch(true, begin, page, rk);
-  PageScale scale = page_scale(a8, head, page), next_scale = page_scale(a8, head, next);
+  look_up(0);
+  fetch(true, k_at, 0, rk);
+  uint64_t absent = gone(0);
   put(true, rk, kt);
   __syncthreads();                                     // (odd_tiles, too)
-  fetch(false, begin, page, rv);
-  fetch(true, begin + C::TN, next, rk);
-  int entry = entry_of(a.pool, b, begin + 2 * C::TN + mine);
+  fetch(false, v_at, 0, rv);
+  fetch(true, k_at, 1, rk);
   f16v even_scores[NB], odd_scores[NB];
-  Groups<NB> g = groups_of(scale);
+  Groups<NB> g = groups_from<NB>(scale, 0);
   c.template scores<NB>(kt, even_scores);
   c.template settle8<NB>(begin, absent, g, even_scores);
-  auto step = [&](int t0, int odd, f16v (&sc)[NB], f16v (&ahead)[NB])
-                  __attribute__((always_inline)) {
+  auto step = [&](int i, int odd, f16v (&sc)[NB], f16v (&next)[NB]) __attribute__((always_inline)) {
     char* const v = vt + odd * C::BYTES;
+    const int t0 = begin + i * C::TN;
     if (absent || t0 + C::TN > wg_hi || t0 < wg_lo) {
       // each thread looks at the values that it has loaded; rows of absent
       // pages become zeros
@@ -837,30 +863,43 @@ __device__ __forceinline__ void many8(const Pt8Args& a8, char* lds, int block) {
     put(false, rv, v);
     put(true, rk, kt + (odd ^ 1) * C::BYTES);
     __syncthreads();                                   // both are there, the other halves free
-    page = next;
-    next = page_at(t0 + 2 * C::TN, entry);
-    absent = next_absent;
-    next_absent = __ballot(next < 0);
+    absent = gone(i + 1);
     const Groups<NB> now = g;
-    scale = next_scale;
-    g = groups_of(scale);
+    g = groups_from<NB>(scale, GP * ((i + 1) % TILES));
     if (t0 + C::TN < end) {
-      fetch(false, t0 + C::TN, page, rv);
-      fetch(true, t0 + 2 * C::TN, next, rk);
-      next_scale = page_scale(a8, head, next);
-      entry = entry_of(a.pool, b, t0 + 3 * C::TN + mine);
+      fetch(false, v_at, i + 1, rv);
+      if ((i + 2) % TILES == 0) look_up(i + 2);        // (what the tiles before want of it is taken)
+      fetch(true, k_at, i + 2, rk);
     }
     // (past the last tile the scores are those of keys that nobody sees)
     typename Vec<T>::v8 p[NB][2];
-    c.template scores<NB>(kt + (odd ^ 1) * C::BYTES, ahead);
+    c.template scores<NB>(kt + (odd ^ 1) * C::BYTES, next);
     c.template weights8<NB>(now, sc, p);
     c.template add_values<NB>(v, p);
-    if (t0 + C::TN < end) c.template settle8<NB>(t0 + C::TN, absent, g, ahead);
+    // (one product of the scores, one key read, and a share of the weights in turn;
+    // then the values, read two products ahead: 1024 tokens over 40000 778 us without
+    // and 748 with it)
+    constexpr int N = NB * (HD / 16), W = NB * 16;     // products, weights
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if (i < N - 2) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 2 * W / N, 0);
+      __builtin_amdgcn_sched_group_barrier(0x400, W / N, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if (i < N - 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
+    if (t0 + C::TN < end) c.template settle8<NB>(t0 + C::TN, absent, g, next);
   };
-  for (int t0 = begin; t0 < end; t0 += 2 * C::TN) {
-    step(t0, 0, even_scores, odd_scores);
-    if (t0 + C::TN >= end) break;
-    step(t0 + C::TN, 1, odd_scores, even_scores);
+  for (int i = 0; begin + i * C::TN < end; i += 2) {
+    step(i, 0, even_scores, odd_scores);
+    if (begin + (i + 1) * C::TN >= end) break;
+    step(i + 1, 1, odd_scores, even_scores);
   }
   __syncthreads();
   const float2 ls = both_halves(c.l);
@@ -898,8 +937,12 @@ __device__ __forceinline__ void few8(const Pt8Args& a8, char* lds, int block) {
   const PtArgs& a = a8.p;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int head = block % a.pool.Hkv;
-  const int rest = block / a.pool.Hkv;
+  // the heads of a piece's tokens, which lie side by side, 8 workgroups apart: on
+  // one XCD, and at the same time
+  const int Hkv = a.pool.Hkv, whole = a.pool.B * a.ns_few / 8 * 8 * Hkv;
+  const int in = block < whole ? block % (8 * Hkv) : block - whole;
+  const int head = block < whole ? in / 8 : in % Hkv;
+  const int rest = block < whole ? block / (8 * Hkv) * 8 + in % 8 : whole / Hkv + in / Hkv;
   const int part = rest % a.ns_few, b = rest / a.ns_few;
   const Seq s = sequence(a, b);
   if (s.n == 0 || !is_few(a, s)) return;
@@ -909,35 +952,36 @@ __device__ __forceinline__ void few8(const Pt8Args& a8, char* lds, int block) {
   const int end = min(w.hi, w.lo + (part + 1) * w.step);
   char* kt = lds + wave * 2 * C::FEW_BYTES;
   char* vt = kt + C::FEW_BYTES;
+  // Pages and scales are looked up for several tiles at once, one group of 8
+  // tokens (which lie in one page) a lane, lane GP (tile mod TILES) + group.  The
+  // table is read a lookup ahead, and the scales of its pages half a lookup:
+  // waiting for either holds up all loads behind it.
+  const int lrow = lane / C::CH, lch = lane % C::CH;
+  const char* const kbase = a.pool.k + head * a.pool.ks[2];
+  const char* const vbase = a.pool.v + head * a.pool.vs[2];
+  auto token_of = [&](int i) { return begin + (i + lane / GP) * C::UNIT + 8 * (lane % GP); };
+  auto page_at = [&](int i, int entry) {
+    return token_of(i) < end ? checked(a.pool, entry) : -1;
+  };
+  int next_entry = entry_of(a.pool, b, token_of(0));
   Columns8<T, HD> c;
   c.template start<true>(a, s, head, lane & 31);
   // keys that every query of the sequence sees
   const int64_t q_hi = min((int64_t)s.keys, s.pos0 + 1);
   const int64_t q_lo = a.window ? s.pos0 + s.n - a.window : 0;
-
-  // Pages and scales are looked up for several tiles at once, one group of 8
-  // tokens (which lie in one page) a lane, lane GP (tile mod TILES) + group.
-  const int lrow = lane / C::CH, lch = lane % C::CH;
-  const char* const kbase = a.pool.k + head * a.pool.ks[2];
-  const char* const vbase = a.pool.v + head * a.pool.vs[2];
   uint64_t k_at = 0, v_at = 0, there = 0;              // offsets; lanes whose page is there
-  PageScale scale = {1.f, 0.f};
+  PageScale scale = {1.f, 0}, next_scale = page_scale(a8, head, page_at(0, next_entry));
   auto look_up = [&](int i) __attribute__((always_inline)) {
-    const int t = begin + (i + lane / GP) * C::UNIT + 8 * (lane % GP);
-    const int page = t < end ? checked(a.pool, entry_of(a.pool, b, t)) : -1;
+    const int t = token_of(i), page = page_at(i, next_entry);
     k_at = token_offset8(a.pool, a.pool.ks, page, t);
     v_at = token_offset8(a.pool, a.pool.vs, page, t);
-    scale = page_scale(a8, head, page);
     there = __ballot(page >= 0);
+    scale = next_scale;
+    if (begin + (i + TILES) * C::UNIT < end)
+      next_entry = entry_of(a.pool, b, token_of(i + TILES));
   };
-  // rows of tile i that are not there: by groups, and behind the last key
   auto gone = [&](int i, int t0) {
-    const uint32_t groups = (uint32_t)(there >> (GP * (i % TILES))) & ((1u << GP) - 1u);
-    uint64_t held = ((groups & 15u) * 0x00204081u & 0x01010101u) * 0xffu;
-    if (NB == 2) held |= (uint64_t)(((groups >> 4) * 0x00204081u & 0x01010101u) * 0xffu) << 32;
-    const uint64_t all = ~0ull >> (64 - C::FEW_N);
-    const int left = end - t0;
-    return (~held | (left >= C::FEW_N ? 0ull : left <= 0 ? ~0ull : ~0ull << left)) & all;
+    return gone_rows<C::FEW_N>((uint32_t)(there >> (GP * (i % TILES))), end - t0);
   };
   auto fetch = [&](bool key, int i, const char* to) __attribute__((always_inline)) {
     const int64_t (&st)[3] = key ? a.pool.ks : a.pool.vs;
@@ -951,13 +995,7 @@ __device__ __forceinline__ void few8(const Pt8Args& a8, char* lds, int block) {
     }
   };
   auto groups_of = [&](int i) __attribute__((always_inline)) {
-    Groups<NB> g;
-#pragma unroll
-    for (int j = 0; j < GP; ++j) {
-      g.ck[j] = of_lane(scale.ck, GP * (i % TILES) + j);
-      g.ev[j] = of_lane(scale.ev, GP * (i % TILES) + j);
-    }
-    return g;
+    return groups_from<NB>(scale, GP * (i % TILES));
   };
   int odd_from = INT32_MAX, odd_to = -1;               // tiles with NaN among the values
   // Keys and values have one tile's place each: while weights are computed
@@ -967,9 +1005,9 @@ __device__ __forceinline__ void few8(const Pt8Args& a8, char* lds, int block) {
   if (begin < end) {
     look_up(0);
     absent = gone(0, begin);
-    g = groups_of(0);
     fetch(true, 0, kt);
     fetch(false, 0, vt);
+    g = groups_of(0);
   }
   int i = 0;
   for (int t0 = begin; t0 < end; t0 += C::UNIT) {
@@ -980,7 +1018,10 @@ __device__ __forceinline__ void few8(const Pt8Args& a8, char* lds, int block) {
     c.template settle8<NB>(t0, absent, g, sc);
     c.template weights8<NB>(g, sc, p);
     wait_lds();                                        // the keys have been read
-    if (++i % TILES == 0) look_up(i);
+    ++i;
+    if (i % TILES == TILES / 2 && t0 + (TILES / 2 + 1) * C::UNIT < end)
+      next_scale = page_scale(a8, head, page_at(i + TILES / 2, next_entry));
+    if (i % TILES == 0) look_up(i);
     fetch(true, i, kt);
     wait_loads<C::FEW_PER>();                          // the values are there
     if (absent || t0 + C::FEW_N > q_hi || t0 < q_lo) {
