@@ -554,7 +554,8 @@ typedef struct {
  * A page that a call writes from two rows of the table holds anything
  * afterwards.
  *
- *  q_out, q_dtype    queries [T][Hq][head_dim], float16 or bfloat16.
+ *  q_out, q_dtype    queries [T][Hq][head_dim], float16 or bfloat16; q_out may
+ *                    be q itself where the types agree and q is dense.
  *  other arguments   as gsrq_paged_append.
  */
 gsrq_status gsrq_paged_append8(const gsrq_pages* pages, const gsrq_page_exps* exps, int64_t T,
@@ -644,8 +645,9 @@ typedef struct {
  *     seq_len[b] becomes L' for them and those that shrink.  A sequence that
  *     was not served has no rows and keeps its length.
  *  4. Row q_start[b] + i is at position p = L + i: slots[row] = page *
- *     page_size + p % page_size, its place among a dense pool's tokens, and
- *     positions[row] = p.  Rows of no sequence, up to T, get -1 in both.
+ *     page_size + p % page_size, its place among a dense pool's tokens (-1 where
+ *     the page is absent), and positions[row] = p.  Rows of no sequence, up to
+ *     T, get -1 in both.
  *
  *  table             [B][ldt] int32, in and out; entries past a sequence's
  *                    pages are neither read nor kept.

@@ -118,7 +118,11 @@ template <typename F> __device__ __forceinline__ void turned(F& lo, F& hi, F c, 
   hi = y * c + x * s;
 }
 
-// The turns of a lane's 8 pairs at a position.
+// The turns of a lane's 8 pairs at a token of a page: those of each eighth token
+// and of the eight steps from it on come from LDS, a product of two for each
+// token (25540 rows of 8 heads in 64 tokens a page: 88 us with a sine and cosine
+// for each, 68 so).  The angle is still that of 64 bits, c and s carry six
+// roundings.
 struct Turns {
   float c[8], s[8];
   __device__ __forceinline__ void at(int64_t pos, const double* theta) {
@@ -126,6 +130,14 @@ struct Turns {
     for (int j = 0; j < 8; ++j) {
       turn_of(pos, theta[j], c[j], s[j]);
       __builtin_amdgcn_sched_barrier(0);             // (one after another: in few registers)
+    }
+  }
+  __device__ __forceinline__ void from(const float2* far, const float2* near) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float2 x = far[j], y = near[j];
+      c[j] = x.x * y.x - x.y * y.y;
+      s[j] = x.y * y.x + x.x * y.y;
     }
   }
 };
@@ -195,6 +207,9 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
   __shared__ unsigned long long top64[E8_THREADS];
   __shared__ int was[E8_THREADS], now[E8_THREADS];
   __shared__ int close, risen;
+  constexpr int HALF = HD / 2, EIGHTHS = E8_KEEP * RP / 8;    // (of the most tokens that are kept)
+  __shared__ float2 far[EIGHTHS][HALF], near[8][HALF];
+  __shared__ float weight[HD];                                // of the norm
   const int tid = threadIdx.x, lane = tid & 63, l = tid % L, row = tid / L;
   const int sub = (int)(wg % (2 * a.groups));
   const int64_t slot = wg / (2 * a.groups);
@@ -243,19 +258,26 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
     h = wide ? head0 + i * beside : i % w.heads;
     return i < items && t < w.tokens && h < w.heads && (!wide || head0 < beside);
   };
-  auto numbers_of = [&](const Raw<TI>& x, int t, int& turned_to, Turns& turns, float (&lo)[8],
-                        float (&hi)[8]) __attribute__((always_inline)) {
+  // `factor`: of the norm, taken where it is `unknown`
+  auto numbers_of = [&](const Raw<TI>& x, int t, int& turned_to, Turns& turns, bool kept,
+                        bool unknown, float& factor, float (&lo)[8], float (&hi)[8])
+                        __attribute__((always_inline)) {
+    asm volatile("" : : : "memory");                   // (weights are read anew, not kept in registers)
     x.get(lo, hi);
     if (w.norm) {
-      const float r = norm_factor<float, HD>(lo, hi, w.eps);
+      if (unknown) factor = norm_factor<float, HD>(lo, hi, w.eps);
+      const float r = factor;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        lo[j] *= r * w.norm[8 * l + j];
-        hi[j] *= r * w.norm[HD / 2 + 8 * l + j];
+        lo[j] *= r * weight[8 * l + j];
+        hi[j] *= r * weight[HALF + 8 * l + j];
       }
     }
     if (w.theta) {
-      if (t != turned_to) turns.at(w.pos + t, w.theta + 8 * l);
+      if (t != turned_to) {
+        if (kept) turns.from(&far[t / 8][8 * l], &near[t % 8][8 * l]);
+        else turns.at(w.pos + t, w.theta + 8 * l);
+      }
       turned_to = t;
 #pragma unroll
       for (int j = 0; j < 8; ++j) turned(lo[j], hi[j], turns.c[j], turns.s[j]);
@@ -297,7 +319,17 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
     was[h] = held_exp(exps[h * es[1]]);
   }
   if (tid == 0) close = risen = 0;
+  if (w.norm && tid < HD) weight[tid] = w.norm[tid];
+  if (keep && w.theta) {
+    const int eighths = (w.tokens + 7) / 8, all = eighths + min(8, w.tokens);
+    for (int i = tid; i < all * HALF; i += E8_THREADS) {
+      const int j = i % HALF, t = i / HALF;
+      float2* to = t < eighths ? &far[t][j] : &near[t - eighths][j];
+      turn_of(t < eighths ? w.pos + 8 * t : t - eighths, w.theta[j], to->x, to->y);
+    }
+  }
   __syncthreads();
+  float factor[E8_KEEP];
   Turns turns;
   int turned_to = -1;
   float lo[8], hi[8];
@@ -306,7 +338,7 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
     for (int i = 0; i < E8_KEEP; ++i) {
       int t, h;
       if (item(i, t, h)) {
-        numbers_of(kept[i], t, turned_to, turns, lo, hi);
+        numbers_of(kept[i], t, turned_to, turns, true, true, factor[i], lo, hi);
         search(h, lo, hi);
       }
     }
@@ -316,12 +348,12 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
       if (!item(i, t, h)) continue;
       Raw<TI> x;
       x.load(w.src + t * w.st0 + h * w.st1 + 8 * l, HD / 2);
-      numbers_of(x, t, turned_to, turns, lo, hi);
+      numbers_of(x, t, turned_to, turns, false, true, factor[0], lo, hi);
       search(h, lo, hi);
     }
   }
   __syncthreads();
-  // An exponent that the roundings of norm and rotation (2^-21 of a, at the most)
+  // An exponent that the roundings of norm and rotation (2^-19 of a, at the most)
   // could change is taken from 64-bit numbers.
   for (int h = tid; h < w.heads; h += E8_THREADS) {
     const float m = __uint_as_float(top[h]);
@@ -347,7 +379,7 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
     for (int i = 0; i < E8_KEEP; ++i) {
       int t, h;
       if (item(i, t, h)) {
-        numbers_of(kept[i], t, turned_to, turns, lo, hi);
+        numbers_of(kept[i], t, turned_to, turns, true, false, factor[i], lo, hi);
         round(t, h, lo, hi);
       }
     }
@@ -357,7 +389,7 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
       if (!item(i, t, h)) continue;
       Raw<TI> x;
       x.load(w.src + t * w.st0 + h * w.st1 + 8 * l, HD / 2);
-      numbers_of(x, t, turned_to, turns, lo, hi);
+      numbers_of(x, t, turned_to, turns, false, true, factor[0], lo, hi);
       round(t, h, lo, hi);
     }
   }
@@ -1113,8 +1145,10 @@ __device__ __forceinline__ void few8(const Pt8Args& a8, char* lds, int block) {
   }
 }
 
+// (Two workgroups a CU also for heads of 64: in the registers of three, chunks
+// spill; 1024 tokens over 30000 took 291 us against 228.)
 template <typename T, int HD>
-__global__ void __launch_bounds__(PT_THREADS, HD == 256 ? 1 : HD == 128 ? 2 : 3) cache8_attn_kernel(Pt8Args a) {
+__global__ void __launch_bounds__(PT_THREADS, HD == 256 ? 1 : 2) cache8_attn_kernel(Pt8Args a) {
   __shared__ __align__(16) char lds[Pt8Cfg<HD>::LDS];
   const bool first = (int)blockIdx.x < a.p.first_blocks;
   const int block = first ? blockIdx.x : blockIdx.x - a.p.first_blocks;

@@ -1,7 +1,8 @@
 // Private header of the paged cache's translation units (gsrq_paged.hip:
-// appending and restoring; gsrq_attn_paged.hip: attention over the pages):
-// the pool of pages as the kernels see it, host checks, and the search for a
-// row's sequence.
+// appending and restoring; gsrq_attn_paged.hip: attention over the pages;
+// gsrq_cache8.hip: both over 8-bit pages; gsrq_serving.hip: planning and drafts):
+// the pool of pages as the kernels see it, host checks, the search for a
+// row's sequence, and accesses to its elements.
 #ifndef GSRQ_PAGED_H
 #define GSRQ_PAGED_H
 

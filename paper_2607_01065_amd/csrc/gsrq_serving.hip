@@ -24,6 +24,7 @@ namespace {
 
 constexpr int PL_THREADS = 1024;
 constexpr int PL_MOST = 8192;             // sequences of a call
+constexpr int PL_EACH = 4;                // entries that a thread moves at once (64 / waves)
 
 struct PlanArgs {
   int32_t *table, *free, *n_free, *seq_len;
@@ -41,33 +42,36 @@ __device__ __forceinline__ int sum_of(int a, int b) {
   return s > (uint32_t)INT32_MAX ? INT32_MAX : (int)s;
 }
 
+// The sums of x up to and with this lane's.
+__device__ __forceinline__ int2 lane_sums(int2 x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x.x, d), z = __shfl_up(x.y, d);
+    x.x = lane >= d ? sum_of(x.x, y) : x.x;
+    x.y = lane >= d ? sum_of(x.y, z) : x.y;
+  }
+  return x;
+}
+
 // The sums of the threads' x in front of this one, and of all (in `all`); for
 // the whole workgroup, of whole waves.
 __device__ __forceinline__ int2 sums_before(int2 x, int2* wave_sums, int2& all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  int2 s = x;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(s.x, d), z = __shfl_up(s.y, d);
-    s.x = lane >= d ? sum_of(s.x, y) : s.x;
-    s.y = lane >= d ? sum_of(s.y, z) : s.y;
-  }
+  const int2 s = lane_sums(x);
   const int up = __shfl_up(s.x, 1), up2 = __shfl_up(s.y, 1);
-  int2 before = make_int2(lane ? up : 0, lane ? up2 : 0);
+  const int2 before = make_int2(lane ? up : 0, lane ? up2 : 0);
   if (waves == 1) {
     all = make_int2(__shfl(s.x, 63), __shfl(s.y, 63));
     return before;
   }
   if (lane == 63) wave_sums[wave] = s;
   __syncthreads();
-  all = make_int2(0, 0);
-  for (int i = 0; i < waves; ++i) {
-    const int2 y = wave_sums[i];
-    if (i < wave) before = make_int2(sum_of(before.x, y.x), sum_of(before.y, y.y));
-    all = make_int2(sum_of(all.x, y.x), sum_of(all.y, y.y));
-  }
+  const int2 sums = lane_sums(lane < waves ? wave_sums[lane] : make_int2(0, 0));
+  all = make_int2(__shfl(sums.x, 63), __shfl(sums.y, 63));
+  const int w = __shfl(sums.x, wave ? wave - 1 : 0), w2 = __shfl(sums.y, wave ? wave - 1 : 0);
   __syncthreads();
-  return before;
+  return wave ? make_int2(sum_of(before.x, w), sum_of(before.y, w2)) : before;
 }
 
 // What a sequence asks for.
@@ -88,34 +92,43 @@ __device__ __forceinline__ Ask ask_of(const PlanArgs& a, int b) {
   return x;
 }
 
-// The last i of first[0 .. n] (ascending, first[0] = 0) with first[i] <= x.
-template <typename P> __device__ __forceinline__ int owner(const P* first, int n, int x) {
-  int lo = 0, hi = n;             // (first[n] is the sum of all: x is below it)
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first[mid] <= x) lo = mid;
-    else hi = mid;
+// For each x the last i < n with first[i] <= x (first ascends from 0): E searches
+// side by side.
+template <int E>
+__device__ __forceinline__ void owners(const int* first, int n, const int (&x)[E], int (&b)[E]) {
+#pragma unroll
+  for (int u = 0; u < E; ++u) b[u] = 0;
+  for (int w = 1 << (31 - __clz(n)); w; w >>= 1) {
+#pragma unroll
+    for (int u = 0; u < E; ++u) {
+      const int i = b[u] + w;
+      const bool fits = i < n && first[i < n ? i : 0] <= x[u];
+      b[u] = fits ? i : b[u];
+    }
   }
-  return lo;
 }
 
-__device__ __forceinline__ void write_slot(const PlanArgs& a, int row) {
-  if (row >= a.q_start[a.B]) {
+// `start`: q_start, or a copy of it.
+__device__ __forceinline__ void write_slot(const PlanArgs& a, const int* start, int row) {
+  if (row >= start[a.B]) {
     a.slots[row] = -1;
     a.positions[row] = -1;
     return;
   }
-  const int b = owner(a.q_start, a.B, row);
-  const int pos = a.seq_len[b] - (a.q_start[b + 1] - row);
+  int own[1];
+  owners<1>(start, a.B, {row}, own);
+  const int b = own[0], pos = a.seq_len[b] - (start[b + 1] - row);
   const int page = a.table[b * a.ldt + (pos >> a.shift)];
   a.slots[row] = page < 0 ? -1 : ((int64_t)page << a.shift) + (pos & ((1 << a.shift) - 1));
   a.positions[row] = pos;
 }
 
 __global__ void __launch_bounds__(PL_THREADS) plan_update_kernel(PlanArgs a, int rows_too) {
-  __shared__ int first[PL_MOST + 1], who[PL_MOST];
+  __shared__ int first[PL_MOST + 1], who[PL_MOST], start[PL_MOST + 1];
   __shared__ int2 wave_sums[PL_THREADS / 64];
+  __shared__ int counts[64];
   const int tid = threadIdx.x, NT = blockDim.x;
+  const int lane = tid & 63, wave = tid >> 6, waves = NT >> 6;
   int count = *a.n_free;
   // pages that are given back: how many entries each sequence has of them
   int base = 0;
@@ -126,7 +139,10 @@ __global__ void __launch_bounds__(PL_THREADS) plan_update_kernel(PlanArgs a, int
     if (b < a.B) q = ask_of(a, b);
     int2 all;
     const int2 before = sums_before(make_int2(max(q.old_pages - q.new_pages, 0), 0), wave_sums, all);
-    if (b < a.B) first[b] = sum_of(base, before.x);
+    if (b < a.B) {
+      first[b] = sum_of(base, before.x);
+      who[b] = q.new_pages;
+    }
     base = sum_of(base, all.x);
   }
   count = count < 0 ? 0 : (count > a.F ? a.F : count);
@@ -135,22 +151,59 @@ __global__ void __launch_bounds__(PL_THREADS) plan_update_kernel(PlanArgs a, int
     __syncthreads();
     // from the last entry to the first, so that taking as many again brings them
     // in the order of the sequences; entries without a page are left out
-    for (int i0 = 0; i0 < base; i0 += NT) {
-      const int i = base - 1 - i0 - tid;
-      int page = -1;
-      if (i >= 0) {
-        const int b = owner(first, a.B, i);
-        const Ask x = ask_of(a, b);
-        int32_t* entry = a.table + b * a.ldt + x.new_pages + (i - first[b]);
-        page = *entry;
-        *entry = -1;
+    // (neighbours in neighbouring threads, one access for a wave's; the next
+    // entries are read before these are stored: a load waits for the stores
+    // before it)
+    int32_t* next[PL_EACH];
+    int next_page[PL_EACH];
+    auto read = [&](int i0) __attribute__((always_inline)) {
+      int at[PL_EACH], own[PL_EACH];
+#pragma unroll
+      for (int u = 0; u < PL_EACH; ++u) at[u] = base - 1 - i0 - (u * NT + tid);
+      owners<PL_EACH>(first, a.B, at, own);
+#pragma unroll
+      for (int u = 0; u < PL_EACH; ++u) {
+        const int b = own[u];
+        next[u] = at[u] >= 0 ? a.table + b * a.ldt + who[b] + (at[u] - first[b]) : nullptr;
+        next_page[u] = next[u] ? *next[u] : -1;
       }
-      int2 all;
-      const int at = sums_before(make_int2(page >= 0, 0), wave_sums, all).x;
-      if (page >= 0 && count + (int64_t)at < a.F) a.free[count + at] = page;
-      count = (int)min((int64_t)a.F, (int64_t)count + all.x);
+    };
+    read(0);
+    for (int i0 = 0; i0 < base; i0 += NT * PL_EACH) {
+      int32_t* entry[PL_EACH];
+      int page[PL_EACH], rank[PL_EACH];
+#pragma unroll
+      for (int u = 0; u < PL_EACH; ++u) {
+        entry[u] = next[u];
+        page[u] = next_page[u];
+      }
+      if (i0 + NT * PL_EACH < base) read(i0 + NT * PL_EACH);
+#pragma unroll
+      for (int u = 0; u < PL_EACH; ++u)
+        if (entry[u]) *entry[u] = -1;
+      // how many pages lie before: in the wave's step, and in those before it
+#pragma unroll
+      for (int u = 0; u < PL_EACH; ++u) {
+        const uint64_t held = __ballot(page[u] >= 0);
+        rank[u] = (int)__popcll(held & ((1ull << lane) - 1));
+        if (lane == 0) counts[u * waves + wave] = (int)__popcll(held);
+      }
+      __syncthreads();
+      int sum = lane < PL_EACH * waves ? counts[lane] : 0;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(sum, d);
+        sum += lane >= d ? y : 0;
+      }
+      const int before = sum - (lane < PL_EACH * waves ? counts[lane] : 0);
+#pragma unroll
+      for (int u = 0; u < PL_EACH; ++u) {
+        const int64_t at = (int64_t)count + __shfl(before, u * waves + wave) + rank[u];
+        if (page[u] >= 0 && at < a.F) a.free[at] = page[u];
+      }
+      count = (int)min((int64_t)a.F, (int64_t)count + __shfl(sum, 63));
+      __syncthreads();
     }
-    __syncthreads();
   }
   // who fits, in order, and what those who fit take
   int2 asked = make_int2(0, 0), given = make_int2(0, 0);       // pages, rows
@@ -172,31 +225,48 @@ __global__ void __launch_bounds__(PL_THREADS) plan_update_kernel(PlanArgs a, int
     if (b < a.B) {
       first[b] = given.x + own.x;
       who[b] = q.old_pages;
-      a.q_start[b] = given.y + own.y;
+      a.q_start[b] = start[b] = given.y + own.y;
       a.seq_len[b] = served ? q.want : q.had;
     }
     given = make_int2(given.x + all.x, given.y + all.y);
   }
   if (tid == 0) {
     first[a.B] = given.x;
-    a.q_start[a.B] = given.y;
+    a.q_start[a.B] = start[a.B] = given.y;
     *a.n_free = count - given.x;
   }
   __syncthreads();
-  for (int i = tid; i < given.x; i += NT) {
-    const int b = owner(first, a.B, i);
-    int32_t* from = a.free + (count - 1 - i);
-    a.table[b * a.ldt + who[b] + (i - first[b])] = *from;
-    *from = -1;
+  int coming[PL_EACH];
+  auto read = [&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < PL_EACH; ++u)
+      coming[u] = i0 + u * NT < given.x ? a.free[count - 1 - i0 - u * NT] : -1;
+  };
+  read(tid);
+  for (int i0 = tid; i0 < given.x; i0 += NT * PL_EACH) {
+    int i[PL_EACH], own[PL_EACH], page[PL_EACH];
+#pragma unroll
+    for (int u = 0; u < PL_EACH; ++u) {
+      i[u] = i0 + u * NT;
+      page[u] = coming[u];
+    }
+    if (i0 + NT * PL_EACH < given.x) read(i0 + NT * PL_EACH);
+    owners<PL_EACH>(first, a.B, i, own);
+#pragma unroll
+    for (int u = 0; u < PL_EACH; ++u) {
+      if (i[u] >= given.x) break;
+      a.table[own[u] * a.ldt + who[own[u]] + (i[u] - first[own[u]])] = page[u];
+      a.free[count - 1 - i[u]] = -1;
+    }
   }
   if (!rows_too) return;
   __syncthreads();
-  for (int row = tid; row < a.T; row += NT) write_slot(a, row);
+  for (int row = tid; row < a.T; row += NT) write_slot(a, start, row);
 }
 
 __global__ void __launch_bounds__(256) plan_slots_finalize_kernel(PlanArgs a) {
   const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (row < a.T) write_slot(a, (int)row);
+  if (row < a.T) write_slot(a, a.q_start, (int)row);
 }
 
 // ------------------------------------------------------------- verification
@@ -247,8 +317,15 @@ __device__ __forceinline__ int stop_of(const VerifyArgs& a, int b, int& first, b
   return first + n - 1;
 }
 
-// The two weights of token v: of what a rejection leaves, and of the target.
+// 16 bytes of a row, which starts at any element.
+template <typename T> struct Some {
+  static constexpr int N = 16 / sizeof(T);
+  typedef T vec __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
+
+// The two weights of a token: of what a rejection leaves, and of the target.
 template <typename T> struct Weights {
+  static constexpr int N = Some<T>::N;
   const T *p, *q;
   int one;                        // the token that a rejection takes out, where q is null
   bool rejected;
@@ -257,10 +334,37 @@ template <typename T> struct Weights {
     q = a.draft ? (const T*)a.draft + row * a.ldq : nullptr;
     one = rej && !q ? a.tokens[row + 1] : -1;
   }
-  __device__ __forceinline__ void get(int v, double& rest, double& all) const {
-    all = weight_of((double)(float)p[v]);
-    rest = 0.0;
-    if (rejected) rest = q ? weight_of((double)(float)p[v] - (double)(float)q[v]) : v == one ? 0.0 : all;
+  __device__ __forceinline__ void of(int v, double x, double y, double& rest, double& all) const {
+    all = weight_of(x);
+    rest = rejected ? q ? weight_of(x - y) : v == one ? 0.0 : all : 0.0;
+  }
+  // E tokens from v on, those from `end` on of no weight: f(index, rest, all).
+  template <int E, typename F> __device__ __forceinline__ void each(int v, int end, F f) const {
+    static_assert(E % N == 0, "whole loads");
+    const bool both = rejected && q;
+    if (v + E <= end) {
+      typename Some<T>::vec x[E / N], y[E / N] = {};
+#pragma unroll
+      for (int i = 0; i < E / N; ++i) x[i] = *(const typename Some<T>::vec*)(p + v + i * N);
+      if (both) {
+#pragma unroll
+        for (int i = 0; i < E / N; ++i) y[i] = *(const typename Some<T>::vec*)(q + v + i * N);
+      }
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        double rest, all;
+        of(v + i, (double)(float)x[i / N][i % N], (double)(float)y[i / N][i % N], rest, all);
+        f(i, rest, all);
+      }
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      double rest = 0.0, all = 0.0;
+      if (v + i < end)
+        of(v + i, (double)(float)p[v + i], both ? (double)(float)q[v + i] : 0.0, rest, all);
+      f(i, rest, all);
+    }
   }
 };
 
@@ -282,12 +386,14 @@ __global__ void __launch_bounds__(VD_THREADS) verify_sums_kernel(VerifyArgs a) {
   const Weights<T> w(a, row, rejected);
   const int end = min(a.V, (c + 1) * a.chunk);
   double rest = 0.0, all = 0.0;
-  for (int v = c * a.chunk + tid; v < end; v += VD_THREADS) {
-    double x, y;
-    w.get(v, x, y);
-    rest += x;
-    all += y;
-  }
+  // (one 16-byte load of a row a lane and step, next to its neighbours')
+  constexpr int E = Weights<T>::N;
+#pragma unroll 4
+  for (int v = c * a.chunk + tid * E; v < end; v += VD_THREADS * E)
+    w.template each<E>(v, end, [&](int, double x, double y) __attribute__((always_inline)) {
+      rest += x;
+      all += y;
+    });
   rest = wave_sum(rest);
   all = wave_sum(all);
   if ((tid & 63) == 0) {
@@ -355,14 +461,11 @@ __global__ void __launch_bounds__(VD_THREADS) verify_finalize_kernel(VerifyArgs 
     const int begin = c * a.chunk, end = min(a.V, begin + a.chunk);
     for (int v0 = begin; v0 < end; v0 += VD_SPAN) {
       double x[VD_EACH], share = 0.0;
-#pragma unroll
-      for (int i = 0; i < VD_EACH; ++i) {
-        const int v = v0 + tid * VD_EACH + i;
-        double rest = 0.0, full = 0.0;
-        if (v < end) w.get(v, rest, full);
+      w.template each<VD_EACH>(v0 + tid * VD_EACH, end, [&](int i, double rest, double full)
+                                                            __attribute__((always_inline)) {
         x[i] = rejected ? rest : full;
         share += x[i];
-      }
+      });
       const double up = sum_up_to(share), before = __shfl_up(up, 1);
       if (lane == 63) ends[wave] = up;
       __syncthreads();

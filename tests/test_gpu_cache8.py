@@ -224,6 +224,22 @@ def test_positions_that_the_table_does_not_hold():
     _check_append(k, v, None, *_pools(6, 8, 2, 64, "token"), tab, start, lens)
 
 
+def test_queries_in_place_and_another_stream():
+    """q_out is q itself, on a stream that is not the current one."""
+    start, k, v, q, w = _rows([5, 70], 40, 2, 128, torch.bfloat16)
+    tab, lens = R.table(2, 6, 14), torch.tensor([9, 90], dtype=torch.int32)
+    pools = _pools(14, 16, 2, 128, "token")
+    ref = _check_append(k, v, q, *pools, tab, start, lens, _theta(128), *w)
+    dev = [t.cuda() for t in (k, v, pools[0], pools[1], tab, start, lens, q, pools[2], pools[3])]
+    theta, kn, qn = _theta(128).cuda(), w[0].cuda(), w[1].cuda()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = B.paged_append(*dev[:7], q=dev[7], q_out=dev[7], theta=theta, k_norm=kn, q_norm=qn, k_exp=dev[8], v_exp=dev[9], stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert got is dev[7] and torch.equal(got, ref[4])
+    assert torch.equal(_raw(dev[2]), _raw(ref[0])) and torch.equal(_raw(dev[3]), _raw(ref[1]))
+
+
 # ---------------------------------------------------------------- attention
 
 ORDER = ("q", "kp", "vp", "ke", "ve", "tab", "start", "lens")
