@@ -72,6 +72,7 @@ struct Append8Args {
   void* q_out;
   int T, Hq;
   int HG, groups;                     // heads per workgroup, and groups of so many
+  int rows;                           // tokens of a workgroup of queries
   int64_t page_wgs;                   // workgroups of pages; the others turn queries
   float eps;
 };
@@ -230,14 +231,14 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
   const int64_t begin = max(from, index << a.pool.shift);
   const int64_t end = min(pos0 + n, (index + 1) << a.pool.shift);
   if (begin >= end) return;
-  const int page = page_of(a.pool, b, begin);
-  if (page < 0) return;
+  // (the page is looked up while the rows are on their way)
+  const int64_t in_row = begin >> a.pool.shift;
+  const int entry = in_row < a.pool.per ? a.pool.table[b * a.pool.ldt + in_row] : -1;
   const int64_t* st = key ? a.kst : a.vst;
   const int64_t* ps = key ? a.pool.ks : a.pool.vs;
   const int64_t* es = key ? a.exps.ks : a.exps.vs;
   PageRows<TI> w;
   w.src = (const TI*)(key ? a.k : a.v) + (first + (begin - pos0)) * st[0] + h0 * st[1];
-  w.dst = (uint8_t*)(key ? a.pool.k : a.pool.v) + page * ps[0] + h0 * ps[2];
   w.st0 = st[0]; w.st1 = st[1]; w.ps1 = ps[1]; w.ps2 = ps[2];
   w.theta = key ? a.theta : nullptr;
   w.norm = key ? a.k_norm : nullptr;
@@ -246,7 +247,6 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
   w.tokens = (int)(end - begin);
   w.heads = min(a.HG, a.pool.Hkv - h0);
   w.kept = (int)(begin & ((1 << a.pool.shift) - 1));
-  int8_t* exps = (key ? a.exps.k : a.exps.v) + page * es[0] + h0 * es[1];
 
   // item i of this thread; whether there is one (whole for its L lanes)
   const bool wide = w.tokens <= RP;
@@ -313,6 +313,10 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
       if (item(i, t, h)) kept[i].load(w.src + t * w.st0 + h * w.st1 + 8 * l, HD / 2);
     }
   }
+  const int page = checked(a.pool, entry);
+  if (page < 0) return;
+  w.dst = (uint8_t*)(key ? a.pool.k : a.pool.v) + page * ps[0] + h0 * ps[2];
+  int8_t* exps = (key ? a.exps.k : a.exps.v) + page * es[0] + h0 * es[1];
   for (int h = tid; h < w.heads; h += E8_THREADS) {
     top[h] = 0;
     top64[h] = 0;
@@ -412,7 +416,7 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
   }
 }
 
-// Queries: E8_ROWS tokens, a row of lanes per head.  All their loads are on the
+// Queries: E8_ROWS tokens (or one), a row of lanes per head.  All their loads are on the
 // way while the threads share the sines and cosines out among themselves.
 constexpr int E8_ROWS = 4;
 
@@ -422,8 +426,8 @@ __device__ __forceinline__ void append_queries(const Append8Args& a, int64_t wg)
   __shared__ float2 turns[E8_ROWS][HALF];
   const int tid = threadIdx.x, l = tid % L;
   const int per = (a.Hq + RP - 1) / RP;
-  const int row0 = (int)(wg / per) * E8_ROWS, h = (int)(wg % per) * RP + tid / L;
-  const int rows = min(E8_ROWS, a.T - row0);
+  const int row0 = (int)(wg / per) * a.rows, h = (int)(wg % per) * RP + tid / L;
+  const int rows = min(a.rows, a.T - row0);
   const bool mine = h < a.Hq;
   Raw<TI> x[E8_ROWS];
   int64_t pos[E8_ROWS];
@@ -1241,7 +1245,10 @@ gsrq_status gsrq_paged_append8(const gsrq_pages* pages, const gsrq_page_exps* ex
   a.groups = (a.pool.Hkv + a.HG - 1) / a.HG;
   a.page_wgs = ((T >> a.pool.shift) + 2ll * a.pool.B) * 2 * a.groups;
   a.Hq = q ? Hq : 0;
-  const int64_t wgs = a.page_wgs + (T + E8_ROWS - 1) / E8_ROWS * ((a.Hq + rows - 1) / rows);
+  // (one token's queries a workgroup where the GPU holds them all at once)
+  const int64_t wide = (a.Hq + rows - 1) / rows;
+  a.rows = T * wide <= 1024 ? 1 : E8_ROWS;
+  const int64_t wgs = a.page_wgs + (T + a.rows - 1) / a.rows * wide;
   if (wgs > MAX_BLOCKS) return GSRQ_E_UNSUPPORTED;
   a.k = k->data;
   a.v = v->data;

@@ -667,18 +667,20 @@ def _exps(k_exp, v_exp, k_pages):
     """gsrq_page_exps of two tensors [pages, Hkv] of exponents; None without them."""
     if k_exp is None and v_exp is None:
         return None
-    torch = _torch()
     if k_exp is None or v_exp is None:
         raise ValueError("k_exp and v_exp come together")
-    shape = (k_pages.shape[0], k_pages.shape[2]) if k_pages.dim() == 4 else ()
+    int8, shape, index = _torch().int8, k_pages.shape, k_pages.get_device()
+    shape = (shape[0], shape[2]) if len(shape) == 4 else ()
     for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
-        if t.dtype is not torch.int8:
+        if t.dtype is not int8:
             raise TypeError(f"{name} must be int8, not {t.dtype}")
         if t.shape != shape:
             raise ValueError(f"{name} must be [pages, Hkv] of the pages, not {tuple(t.shape)}")
-        if t.get_device() != k_pages.get_device():
+        if t.get_device() != index:
             raise ValueError(f"{name} is on {t.device}, expected {k_pages.device}")
-    return _PAGE_EXPS.pack(k_exp.data_ptr(), v_exp.data_ptr(), *k_exp.stride(), *v_exp.stride())
+    k0, k1 = k_exp.stride()
+    v0, v1 = v_exp.stride()
+    return _PAGE_EXPS.pack(k_exp.data_ptr(), v_exp.data_ptr(), k0, k1, v0, v1)
 
 
 def _heads(x, name, heads, head_dim, rows, dtype, like) -> bytes:
