@@ -335,3 +335,27 @@ def test_captured_step_is_the_eager_one():
             assert torch.equal(x, y)
         for x, y in zip(held, eager):
             assert torch.equal(x.view(torch.uint8) if x.dtype is C.E4M3 else x, y.view(torch.uint8) if y.dtype is C.E4M3 else y)
+
+
+def test_readme_example_of_8_bit_pages():
+    """The block of the README that plans, appends, attends and verifies over 8-bit pages, as it stands there."""
+    import os
+    import re
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    block = next(b for b in re.findall(r"```python\n(.*?)```", text, re.S) if "verify_drafts" in b)
+    n, Hkv, V, counts = 3, 2, 300, [4, 1, 20]
+    T = sum(counts)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    k, v, q = (torch.randn((T, h, 128), generator=g, device="cuda").half() for h in (Hkv, Hkv, 4))
+    target, draft = (torch.rand((T, V), generator=g, device="cuda") for _ in range(2))
+    names = dict(torch=torch, B=B, n=n, per=4, pages=12, Hkv=Hkv, T=T, new=_i32(counts), k=k, v=v, q=q, target=target, draft=draft,
+                 theta=10000.0 ** (torch.arange(64, dtype=torch.float64, device="cuda") * (-2.0 / 128)),
+                 tokens=torch.randint(0, V, (T,), generator=g, device="cuda").int(), uniform=torch.rand(T, generator=g, device="cuda"),
+                 draw=torch.rand(n, generator=g, device="cuda"))
+    exec(block, names)
+    torch.cuda.synchronize()
+    assert names["out"].shape == (T, 4, 128) and torch.all(torch.isfinite(names["out"]))
+    ref = C.verify(names["tokens"].cpu(), target.cpu(), draft.cpu(), names["uniform"].cpu(), names["draw"].cpu(), names["q_start"].cpu())
+    assert names["accepted"].tolist() == ref[0].tolist() and names["next_token"].tolist() == ref[1].tolist()
+    assert names["seq_len"].tolist() == [1 + a for a in names["accepted"].tolist()]
+    assert int(names["n_free"]) == 12 - sum(-(-(1 + a) // 16) for a in names["accepted"].tolist())
