@@ -121,9 +121,9 @@ template <typename F> __device__ __forceinline__ void turned(F& lo, F& hi, F c, 
 
 // The turns of a lane's 8 pairs at a token of a page: those of each eighth token
 // and of the eight steps from it on come from LDS, a product of two for each
-// token (25540 rows of 8 heads in 64 tokens a page: 88 us with a sine and cosine
-// for each, 68 so).  The angle is still that of 64 bits, c and s carry six
-// roundings.
+// token (keys and values of 25540 rows, 8 heads, pages of 64 tokens: 75 us with a
+// sine and cosine for each, 52 so).  The angle is still that of 64 bits, c and s
+// carry six roundings.
 struct Turns {
   float c[8], s[8];
   __device__ __forceinline__ void at(int64_t pos, const double* theta) {
@@ -416,8 +416,8 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
   }
 }
 
-// Queries: E8_ROWS tokens (or one), a row of lanes per head.  All their loads are on the
-// way while the threads share the sines and cosines out among themselves.
+// Queries: E8_ROWS tokens (or one), a row of lanes per head.  All their loads are
+// on the way while the threads share the sines and cosines out among themselves.
 constexpr int E8_ROWS = 4;
 
 template <typename TI, typename TQ, int HD>
@@ -1238,10 +1238,15 @@ gsrq_status gsrq_paged_append8(const gsrq_pages* pages, const gsrq_page_exps* ex
   if (T > MAX_BLOCKS || a.pool.B > (1 << 20)) return GSRQ_E_UNSUPPORTED;
   if (2ll * a.pool.Hkv + (q ? Hq : 0) > 65535) return GSRQ_E_UNSUPPORTED;
   const int hd = pages->head_dim, rows = E8_THREADS * 16 / hd;
-  // as many heads as E8_KEEP items a thread hold of a page's tokens
+  // as many heads as E8_KEEP items a thread hold of a page's tokens; fewer where that
+  // leaves less than 512 workgroups, but for sequences of one token each, whose
+  // heads are few items (512 tokens: 11.9 us with all, 8.7 so; 32 sequences of one
+  // token 6.5 and 7.8)
   const int tokens = (int)std::min<int64_t>(pages->page_size, T);
   const int most = tokens <= rows ? E8_KEEP * (rows / tokens) : E8_KEEP / ((tokens + rows - 1) / rows);
-  a.HG = std::min(a.pool.Hkv, std::max(1, most));
+  const int64_t touched = (T >> a.pool.shift) + a.pool.B;
+  const int64_t fill = T > a.pool.B ? 2 * touched * a.pool.Hkv / 512 : most;
+  a.HG = (int)std::min<int64_t>(a.pool.Hkv, std::max<int64_t>(1, std::min<int64_t>(most, fill)));
   a.groups = (a.pool.Hkv + a.HG - 1) / a.HG;
   a.page_wgs = ((T >> a.pool.shift) + 2ll * a.pool.B) * 2 * a.groups;
   a.Hq = q ? Hq : 0;
