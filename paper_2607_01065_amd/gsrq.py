@@ -664,9 +664,7 @@ def _pages(k_pages, v_pages, table, eight=False) -> bytes:
 
 
 def _exps(k_exp, v_exp, k_pages):
-    """gsrq_page_exps of two tensors [pages, Hkv] of exponents; None without them."""
-    if k_exp is None and v_exp is None:
-        return None
+    """gsrq_page_exps of two tensors [pages, Hkv] of exponents."""
     if k_exp is None or v_exp is None:
         raise ValueError("k_exp and v_exp come together")
     int8, shape, index = _torch().int8, k_pages.shape, k_pages.get_device()
@@ -727,7 +725,7 @@ def paged_append(k, v, k_pages, v_pages, table, q_start, seq_len, *, q=None, the
     the queries come in q_out's type, or else q's, of float32 rows bfloat16."""
     torch = _torch()
     lib = _lib or load_library()
-    exps = _exps(k_exp, v_exp, k_pages)
+    exps = None if k_exp is None is v_exp else _exps(k_exp, v_exp, k_pages)
     pages = _pages(k_pages, v_pages, table, exps is not None)
     B = table.shape[0]
     _, _, Hkv, hd = k_pages.shape
@@ -804,7 +802,7 @@ def attn_paged(q, k_pages, v_pages, table, q_start, seq_len, *, scale=None, wind
     bfloat16."""
     torch = _torch()
     lib = _lib or load_library()
-    exps = _exps(k_exp, v_exp, k_pages)
+    exps = None if k_exp is None is v_exp else _exps(k_exp, v_exp, k_pages)
     pages = _pages(k_pages, v_pages, table, exps is not None)
     if q.dim() != 3:
         raise ValueError("q must be [T, Hq, head_dim]")
@@ -939,10 +937,9 @@ def paged_plan(table, free_pages, n_free, seq_len, change, *, page_size, rows, q
         raise ValueError("a size does not fit 32 bits, or page_size is no number of tokens") from None
 
     def call():
-        dev = table.device
-        out = (torch.empty(B + 1, dtype=torch.int32, device=dev) if q_start is None else q_start,
-               torch.empty(rows, dtype=torch.int64, device=dev) if slots is None else slots,
-               torch.empty(rows, dtype=torch.int32, device=dev) if positions is None else positions)
+        out = (table.new_empty(B + 1) if q_start is None else q_start,
+               table.new_empty(rows, dtype=torch.int64) if slots is None else slots,
+               table.new_empty(rows) if positions is None else positions)
         st = lib.gsrq_paged_plan(s, table.data_ptr(), pool, count, lens, moves, out[0].data_ptr(),
                                  out[1].data_ptr() or None, out[2].data_ptr() or None,
                                  _append_stream_handle(stream))
@@ -1008,14 +1005,13 @@ def verify_drafts(tokens, target, draft, uniform, draw, q_start, *, accepted=Non
         raise ValueError(f"workspace must be contiguous, on {target.device}")
 
     def call():
-        dev = target.device
-        out = (torch.empty(B, dtype=torch.int32, device=dev) if accepted is None else accepted,
-               torch.empty(B, dtype=torch.int32, device=dev) if next_token is None else next_token)
+        out = (q_start.new_empty(B) if accepted is None else accepted,
+               q_start.new_empty(B) if next_token is None else next_token)
         n = ctypes.c_size_t()
         st = lib.gsrq_verify_drafts_workspace_bytes(T, V, B, ctypes.byref(n))
         if st != GSRQ_OK:
             _check(st, "gsrq_verify_drafts_workspace_bytes")
-        ws = _workspace(n.value, dev, workspace)
+        ws = _workspace(n.value, target.device, workspace)
         st = lib.gsrq_verify_drafts(T, V, B, ids or None, target.data_ptr() or None, ld[0],
                                     _ptr(draft), ld[1], dt, u or None, d, start,
                                     out[0].data_ptr(), out[1].data_ptr(), ws.data_ptr(),

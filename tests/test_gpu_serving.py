@@ -139,9 +139,9 @@ def _probabilities(T, V, dtype, seed, near=0.5):
     return p, torch.softmax(x + near * torch.randn((T, V), generator=g), -1).to(dtype), g
 
 
-def _verify(tokens, p, q, u, d, start, **kw):
+def _verify(tokens, p, q, u, d, start):
     ref = C.verify(tokens, p, q, u, d, start)
-    got = B.verify_drafts(tokens.cuda(), p.cuda() if kw.get("move", True) else p, None if q is None else q.cuda(), u.cuda(), d.cuda(), start.cuda())
+    got = B.verify_drafts(tokens.cuda(), p.cuda(), None if q is None else q.cuda(), u.cuda(), d.cuda(), start.cuda())
     torch.cuda.synchronize()
     assert got[0].tolist() == ref[0].tolist(), "accepted"
     assert got[1].tolist() == ref[1].tolist(), "next"
@@ -210,6 +210,20 @@ def test_weights_of_nothing_nan_and_strided_rows():
     got = B.verify_drafts(tokens.cuda(), wide[:, 1:5002], wide[:, 5002:10003], u.cuda(), d.cuda(), start.cuda())
     ref = C.verify(tokens, p.half(), q.half(), u, d, start)
     assert got[0].tolist() == ref[0].tolist() and got[1].tolist() == ref[1].tolist()
+
+
+def test_rows_more_than_2_31_elements_apart():
+    big = torch.zeros((1 << 31) + 2000, dtype=torch.float16, device="cuda")
+    p, q, g = _probabilities(3, 700, torch.float16, 5)
+    far = [big[i:].as_strided((3, 700), (1 << 30, 1)) for i in (0, 1001)]
+    far[0].copy_(p)
+    far[1].copy_(q)
+    tokens, u, d = torch.tensor([0, 9, 600], dtype=torch.int32), torch.tensor([0.1, 0.9, 0.5]), torch.tensor([0.3, 0.7])
+    for start in ([0, 3, 3], [0, 1, 3]):
+        start = torch.tensor(start, dtype=torch.int32)
+        ref = C.verify(tokens, p, q, u, d, start)
+        got = B.verify_drafts(tokens.cuda(), far[0], far[1], u.cuda(), d.cuda(), start.cuda())
+        assert got[0].tolist() == ref[0].tolist() and got[1].tolist() == ref[1].tolist()
 
 
 def test_verify_graph_workspace_and_stream():
