@@ -665,7 +665,7 @@ gsrq_status gsrq_paged_plan(const gsrq_paged_batch* s, int32_t* table, int32_t* 
                             int32_t* n_free, int32_t* seq_len, const int32_t* change,
                             int32_t* q_start, int64_t* slots, int32_t* positions, void* stream);
 
-/* Workspace bytes gsrq_verify_drafts needs. */
+/* Workspace bytes gsrq_verify_drafts needs (0: none). */
 gsrq_status gsrq_verify_drafts_workspace_bytes(int64_t T, int64_t V, int32_t B, size_t* bytes);
 
 /*

@@ -12,8 +12,9 @@
 // drawn from max(p - q, 0), after the last draft from p:
 //   token = min { v : w_0 + .. + w_v > draw * sum w },
 // with all sums in 64 bits (float32 would lose a token's weight in the sum of a
-// vocabulary).  The first launch decides how far a sequence gets and sums its
-// row's weights in chunks; the second finds the chunk and the token in it.
+// vocabulary).  Rows of at most 4096 tokens are one workgroup's; for longer ones
+// a first launch decides how far a sequence gets and sums its row's weights in
+// chunks, and a second finds the chunk and the token in it.
 #include <algorithm>
 
 #include "gsrq_paged.h"
@@ -338,8 +339,8 @@ template <typename T> struct Weights {
     all = weight_of(x);
     rest = rejected ? q ? weight_of(x - y) : v == one ? 0.0 : all : 0.0;
   }
-  // E tokens from v on, those from `end` on of no weight: f(index, rest, all).
-  template <int E, typename F> __device__ __forceinline__ void each(int v, int end, F f) const {
+  // E tokens from v on, those from `end` on as if p and q were zero: f(index, p, q).
+  template <int E, typename F> __device__ __forceinline__ void load(int v, int end, F f) const {
     static_assert(E % N == 0, "whole loads");
     const bool both = rejected && q;
     if (v + E <= end) {
@@ -351,20 +352,37 @@ template <typename T> struct Weights {
         for (int i = 0; i < E / N; ++i) y[i] = *(const typename Some<T>::vec*)(q + v + i * N);
       }
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        double rest, all;
-        of(v + i, (double)(float)x[i / N][i % N], (double)(float)y[i / N][i % N], rest, all);
-        f(i, rest, all);
-      }
+      for (int i = 0; i < E; ++i)
+        f(i, (double)(float)x[i / N][i % N], (double)(float)y[i / N][i % N]);
       return;
+    }
+    // (the last one's place for those behind it: loads without branches, side by side)
+    T x[E], y[E] = {};
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] = p[min(v + i, end - 1)];
+    if (both) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) y[i] = q[min(v + i, end - 1)];
     }
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      double rest = 0.0, all = 0.0;
-      if (v + i < end)
-        of(v + i, (double)(float)p[v + i], both ? (double)(float)q[v + i] : 0.0, rest, all);
-      f(i, rest, all);
+      const bool in = v + i < end;
+      f(i, in ? (double)(float)x[i] : 0.0, in ? (double)(float)y[i] : 0.0);
     }
+  }
+  // Both weights: f(index, rest, all).
+  template <int E, typename F> __device__ __forceinline__ void each(int v, int end, F f) const {
+    load<E>(v, end, [&](int i, double x, double y) __attribute__((always_inline)) {
+      double rest, all;
+      of(v + i, x, y, rest, all);
+      f(i, rest, all);
+    });
+  }
+  // The one that counts (q is zero where none was rejected): f(index, weight).
+  template <int E, typename F> __device__ __forceinline__ void chosen(int v, int end, F f) const {
+    load<E>(v, end, [&](int i, double x, double y) __attribute__((always_inline)) {
+      f(i, v + i == one ? 0.0 : weight_of(x - y));
+    });
   }
 };
 
@@ -516,6 +534,69 @@ __global__ void __launch_bounds__(VD_THREADS) verify_finalize_kernel(VerifyArgs 
   }
 }
 
+// A row of at most VD_ROW tokens by one workgroup, in one launch: sums of
+// neighbours by thread, then the thread that holds the drawn point goes through
+// its share once more.  (Longer rows are too much work in 64 bits for one CU: 4000
+// tokens take 8.1 us so and 8.8 in two launches, which cost the caller 3 us more;
+// 8000 took 10.9 and 9.8, 32000 15 and 9.)
+constexpr int VD_MOST = 512, VD_LANE = 8, VD_ROW = VD_MOST * VD_LANE;
+
+template <typename T>
+__global__ void __launch_bounds__(VD_MOST) verify_row_kernel(VerifyArgs a) {
+  __shared__ double ends[VD_MOST / 64];
+  __shared__ int hit, last;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int first;
+  bool rejected;
+  const int row = stop_of<T>(a, b, first, rejected);
+  if (tid == 0) {
+    a.accepted[b] = row < 0 ? 0 : row - first;
+    a.next[b] = -1;
+    hit = INT32_MAX;
+    last = -1;
+  }
+  if (row < 0) return;
+  Weights<T> w(a, row, rejected);
+  double x[VD_LANE], share, up, from, total;
+  for (;;) {
+    share = 0.0;
+    w.template chosen<VD_LANE>(tid * VD_LANE, a.V, [&](int i, double y) __attribute__((always_inline)) {
+      x[i] = y;
+      share += y;
+    });
+    up = sum_up_to(share);
+    if (lane == 63) ends[wave] = up;
+    __syncthreads();
+    from = total = 0.0;
+    for (int i = 0; i < (int)(blockDim.x >> 6); ++i) {
+      from = i == wave ? total : from;
+      total += ends[i];
+    }
+    if (!w.rejected || total > 0.0) break;
+    w = Weights<T>(a, row, false);                     // (p <= q everywhere: from p)
+    __syncthreads();
+  }
+  const double point = (double)a.draw[b] * total, in = __shfl_up(up, 1);
+  if (share > 0.0) {
+    atomicMax(&last, tid);
+    if (from + up > point) atomicMin(&hit, tid);
+  }
+  __syncthreads();
+  if (tid != (hit < INT32_MAX ? hit : last)) return;
+  // the token that passes the point, or the last of any weight
+  double at = from + (lane ? in : 0.0);
+  int here = -1, heavy = 0;
+#pragma unroll
+  for (int i = 0; i < VD_LANE; ++i) {
+    at += x[i];
+    if (x[i] > 0.0) {
+      heavy = i;
+      if (here < 0 && at > point) here = i;
+    }
+  }
+  a.next[b] = tid * VD_LANE + (here >= 0 ? here : heavy);
+}
+
 // Elements of a row that one workgroup sums: 4096 and more, a power of two, in
 // at most 64 chunks.
 void verify_chunks(int64_t V, int& chunk, int& chunks) {
@@ -525,7 +606,8 @@ void verify_chunks(int64_t V, int& chunk, int& chunks) {
   chunks = (int)((V + c - 1) / c);
 }
 
-size_t verify_bytes(int64_t B, int chunks) {
+size_t verify_bytes(int64_t V, int64_t B, int chunks) {
+  if (V <= VD_ROW) return 0;
   return align256((size_t)B * sizeof(int4)) + align256((size_t)B * 2 * chunks * sizeof(double));
 }
 
@@ -537,6 +619,11 @@ gsrq_status verify_shape(int64_t T, int64_t V, int64_t B) {
 
 template <typename T> gsrq_status verify_launch(const VerifyArgs& a, hipStream_t st) {
   TimedLaunch tl(GSRQ_KERNEL_SERVING, st);
+  if (a.V <= VD_ROW) {
+    const int threads = ((a.V + VD_LANE - 1) / VD_LANE + 63) / 64 * 64;
+    verify_row_kernel<T><<<(unsigned)a.B, threads, 0, st>>>(a);
+    return launch_ok();
+  }
   verify_sums_kernel<T><<<(unsigned)a.B * (unsigned)a.chunks, VD_THREADS, 0, st>>>(a);
   gsrq_status e = launch_ok();
   if (e) return e;
@@ -594,7 +681,7 @@ gsrq_status gsrq_verify_drafts_workspace_bytes(int64_t T, int64_t V, int32_t B, 
   if (e) return e;
   int chunk, chunks;
   verify_chunks(V, chunk, chunks);
-  *bytes = verify_bytes(B, chunks);
+  *bytes = verify_bytes(V, B, chunks);
   return GSRQ_OK;
 }
 
@@ -605,16 +692,17 @@ gsrq_status gsrq_verify_drafts(int64_t T, int64_t V, int32_t B, const int32_t* t
                                void* workspace, size_t ws_bytes, void* stream) {
   gsrq_status e = verify_shape(T, V, B);
   if (e) return e;
-  if (!q_start || !draw || !accepted || !next || !workspace) return GSRQ_E_ARG;
+  if (!q_start || !draw || !accepted || !next) return GSRQ_E_ARG;
   if (T > 0 && (!tokens || !target || !uniform)) return GSRQ_E_ARG;
   if (T > 1 && (ldp < V || (draft && ldq < V))) return GSRQ_E_ARG;
   if (dtype != GSRQ_F32 && dtype != GSRQ_F16 && dtype != GSRQ_BF16) return GSRQ_E_ARG;
   const uintptr_t esz = dtype == GSRQ_F32 ? 4 : 2;
-  if ((uintptr_t)target % esz || (uintptr_t)draft % esz || (uintptr_t)workspace % 256)
-    return GSRQ_E_ARG;
+  if ((uintptr_t)target % esz || (uintptr_t)draft % esz) return GSRQ_E_ARG;
   VerifyArgs a;
   verify_chunks(V, a.chunk, a.chunks);
-  if (ws_bytes < verify_bytes(B, a.chunks)) return GSRQ_E_WORKSPACE;
+  const size_t bytes = verify_bytes(V, B, a.chunks);
+  if (bytes && (!workspace || (uintptr_t)workspace % 256)) return GSRQ_E_ARG;
+  if (ws_bytes < bytes) return GSRQ_E_WORKSPACE;
   a.tokens = tokens;
   a.q_start = q_start;
   a.target = target;

@@ -1011,11 +1011,14 @@ def verify_drafts(tokens, target, draft, uniform, draw, q_start, *, accepted=Non
         st = lib.gsrq_verify_drafts_workspace_bytes(T, V, B, ctypes.byref(n))
         if st != GSRQ_OK:
             _check(st, "gsrq_verify_drafts_workspace_bytes")
-        ws = _workspace(n.value, target.device, workspace)
+        ws, size = None, n.value
+        if size:
+            ws = _workspace(size, target.device, workspace)
+            size = ws.numel() * ws.element_size()
         st = lib.gsrq_verify_drafts(T, V, B, ids or None, target.data_ptr() or None, ld[0],
                                     _ptr(draft), ld[1], dt, u or None, d, start,
-                                    out[0].data_ptr(), out[1].data_ptr(), ws.data_ptr(),
-                                    ws.numel() * ws.element_size(), _append_stream_handle(stream))
+                                    out[0].data_ptr(), out[1].data_ptr(), _ptr(ws), size,
+                                    _append_stream_handle(stream))
         if st != GSRQ_OK:
             _check(st, "gsrq_verify_drafts")
         return out

@@ -105,6 +105,9 @@ def test_plan_refuses(kw, status):
     assert _plan(**kw) == status
 
 
+LARGE = dict(V=50000, ldp=50000, ldq=50000)          # (fewer tokens need no workspace)
+
+
 def _verify(T=10, V=100, Bn=2, tokens=PTR, target=PTR, ldp=100, draft=PTR, ldq=100, dtype=B.GSRQ_F32, uniform=PTR, draw=PTR,
             q_start=PTR, accepted=PTR, nxt=PTR, ws=PTR, nbytes=1 << 30):
     return B.load_library().gsrq_verify_drafts(T, V, Bn, tokens, target, ldp, draft, ldq, dtype, uniform, draw, q_start, accepted,
@@ -115,7 +118,7 @@ def _verify(T=10, V=100, Bn=2, tokens=PTR, target=PTR, ldp=100, draft=PTR, ldq=1
     (dict(T=-1), 1), (dict(V=0), 1), (dict(Bn=0), 1), (dict(Bn=(1 << 16) + 1), 2), (dict(V=1 << 31), 2), (dict(T=1 << 31), 2),
     (dict(tokens=None), 1), (dict(target=None), 1), (dict(uniform=None), 1), (dict(draw=None), 1), (dict(q_start=None), 1),
     (dict(accepted=None), 1), (dict(nxt=None), 1), (dict(ldp=99), 1), (dict(ldq=99), 1), (dict(dtype=3), 1), (dict(target=PTR + 2), 1),
-    (dict(draft=PTR + 1, dtype=B.GSRQ_F16), 1), (dict(ws=None), 1), (dict(ws=PTR + 16), 1), (dict(nbytes=0), 3)])
+    (dict(draft=PTR + 1, dtype=B.GSRQ_F16), 1), (dict(ws=None, **LARGE), 1), (dict(ws=PTR + 16, **LARGE), 1), (dict(nbytes=0, **LARGE), 3)])
 def test_verify_refuses(kw, status):
     assert _verify(**kw) == status
 

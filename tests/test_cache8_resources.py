@@ -25,6 +25,7 @@ WANTED = {
     "gsrq_serving.hip": {
         "plan_update_kernel": (4, 160 * 1024),                     # one workgroup of at most 16 waves
         "verify_sums_kernel": (8, 1024),
+        "verify_row_kernel": (4, 1024),
         "verify_finalize_kernel": (4, 1024),
     },
 }

@@ -150,7 +150,8 @@ def _verify(tokens, p, q, u, d, start):
 
 @pytest.mark.parametrize("counts,V,dtype,draft", [
     ([1], 1, "f32", True), ([2], 7, "f32", True), ([5], 1000, "f16", True), ([5, 0, 1, 8], 4097, "bf16", True),
-    ([3] * 20, 8191, "f32", True), ([4, 9, 2], 32000, "f16", False), ([6] * 5, 100003, "f32", False), ([7, 3], 300001, "bf16", True),
+    ([3] * 20, 8191, "f32", True), ([4, 9, 2], 32000, "f16", False), ([4, 9, 2], 4090, "f32", True), ([3, 5], 4096, "bf16", True), ([3, 5], 4097, "f16", True),
+    ([6] * 5, 100003, "f32", False), ([7, 3], 300001, "bf16", True),
     ([150, 70], 513, "f32", True), ([1] * 300, 100, "f16", True)])
 def test_verify(counts, V, dtype, draft):
     """Ragged drafts; most of what the draft proposes is its own draw, some tokens are unlikely or not in the vocabulary."""
@@ -172,14 +173,17 @@ def test_verify(counts, V, dtype, draft):
 def test_draws_at_the_borders_between_tokens():
     """Sixteenths, whose sums are exact: a draw on a border belongs to the token behind it, at 0 to the first of any weight,
     just below 1 and beyond to the last of any weight."""
-    p = torch.tensor([[0, 4, 0, 8, 0, 4, 0, 0]]) / 16.0
+    short = torch.tensor([[0, 4, 0, 8, 0, 4, 0, 0]]) / 16.0
     want = {0.0: 1, 0.25: 3, 0.25 - 2 ** -20: 1, 0.75: 5, 0.75 - 2 ** -20: 3, 1 - 2 ** -24: 5, 1.0: 5, 7.0: 5, -1.0: 1}
-    for draw, token in want.items():
-        got = B.verify_drafts(_i32([3]), p.cuda(), None, torch.zeros(1, device="cuda"), torch.tensor([draw], device="cuda"), _i32([0, 1]))
-        assert (int(got[0]), int(got[1])) == (0, token), draw
+    for spread in (1, 9000):                               # (both ways to sum)
+        p = torch.zeros((1, 8 * spread))
+        p[0, ::spread] = short[0]
+        for draw, token in want.items():
+            got = B.verify_drafts(_i32([3]), p.cuda(), None, torch.zeros(1, device="cuda"), torch.tensor([draw], device="cuda"), _i32([0, 1]))
+            assert (int(got[0]), int(got[1])) == (0, token * spread), draw
 
 
-@pytest.mark.parametrize("V", [8, 4096, 8193, 70000])
+@pytest.mark.parametrize("V", [8, 4096, 4097, 8193, 70000])
 def test_acceptance_at_its_border(V):
     """u q = p is a rejection, u q just below p none; q = 0 with p above zero stands, p = 0 never; the rest of a rejection
     where p <= q everywhere is p."""
@@ -196,18 +200,19 @@ def test_acceptance_at_its_border(V):
     assert int(ref[0]) == 0 and int(ref[1]) == V - 1
 
 
-def test_weights_of_nothing_nan_and_strided_rows():
-    p, q, g = _probabilities(6, 5001, torch.float32, 3)
+@pytest.mark.parametrize("V", [3001, 50001])
+def test_weights_of_nothing_nan_and_strided_rows(V):
+    p, q, g = _probabilities(6, V, torch.float32, 3)
     p[0], p[1, 7], p[2] = 0.0, float("nan"), float("nan")
     p[3] = -p[3]
     start = torch.tensor([0, 1, 2, 3, 4, 6], dtype=torch.int32)
     tokens, u = torch.zeros(6, dtype=torch.int32), torch.rand(6, generator=g)
     ref = _verify(tokens, p, q, u, torch.rand(5, generator=g), start)
     assert ref[1].tolist()[0] == ref[1].tolist()[2] == ref[1].tolist()[3] == -1
-    wide = torch.zeros((6, 2 * 5001 + 3), device="cuda", dtype=torch.float16)
-    wide[:, 1:5002], wide[:, 5002:10003] = p.half().cuda(), q.half().cuda()       # odd starts and strides
+    wide = torch.zeros((6, 2 * V + 3), device="cuda", dtype=torch.float16)
+    wide[:, 1:V + 1], wide[:, V + 1:2 * V + 1] = p.half().cuda(), q.half().cuda()       # odd starts and strides
     d = torch.rand(5, generator=g)
-    got = B.verify_drafts(tokens.cuda(), wide[:, 1:5002], wide[:, 5002:10003], u.cuda(), d.cuda(), start.cuda())
+    got = B.verify_drafts(tokens.cuda(), wide[:, 1:V + 1], wide[:, V + 1:2 * V + 1], u.cuda(), d.cuda(), start.cuda())
     ref = C.verify(tokens, p.half(), q.half(), u, d, start)
     assert got[0].tolist() == ref[0].tolist() and got[1].tolist() == ref[1].tolist()
 
@@ -226,14 +231,17 @@ def test_rows_more_than_2_31_elements_apart():
         assert got[0].tolist() == ref[0].tolist() and got[1].tolist() == ref[1].tolist()
 
 
-def test_verify_graph_workspace_and_stream():
+@pytest.mark.parametrize("V", [4000, 70001])
+def test_verify_graph_workspace_and_stream(V):
     start, T = R.new_rows([4, 4, 2])
-    p, q, g = _probabilities(T, 9000, torch.float32, 1)
-    tokens = torch.randint(0, 9000, (T,), generator=g).to(torch.int32)
+    p, q, g = _probabilities(T, V, torch.float32, 1)
+    tokens = torch.randint(0, V, (T,), generator=g).to(torch.int32)
     dev = [x.cuda() for x in (tokens, p, q, torch.rand(T, generator=g), torch.rand(3, generator=g), start)]
-    ws = torch.empty(B.verify_drafts_workspace_bytes(T, 9000, 3), dtype=torch.uint8, device="cuda")
-    with pytest.raises(ValueError):
-        B.verify_drafts(*dev, workspace=ws[:64])
+    ws = torch.empty(B.verify_drafts_workspace_bytes(T, V, 3), dtype=torch.uint8, device="cuda")
+    assert (ws.numel() > 0) == (V > 4096)
+    if ws.numel():
+        with pytest.raises(ValueError):
+            B.verify_drafts(*dev, workspace=ws[:64])
     out = [torch.empty(3, dtype=torch.int32, device="cuda") for _ in range(2)]
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
