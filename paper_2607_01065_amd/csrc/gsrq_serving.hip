@@ -43,17 +43,23 @@ __device__ __forceinline__ int sum_of(int a, int b) {
   return s > (uint32_t)INT32_MAX ? INT32_MAX : (int)s;
 }
 
-// The sums of x up to and with this lane's.
-__device__ __forceinline__ int2 lane_sums(int2 x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x.x, d), z = __shfl_up(x.y, d);
-    x.x = lane >= d ? sum_of(x.x, y) : x.x;
-    x.y = lane >= d ? sum_of(x.y, z) : x.y;
-  }
-  return x;
+// One step of a sum over the lanes before: x plus that of the lane that CTRL
+// names, where there is one, in the rows of 16 lanes of ROWS.
+template <int CTRL, int ROWS> __device__ __forceinline__ int step_sum(int x) {
+  return sum_of(x, __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false));
 }
+// The sum of x up to and with this lane's: in rows of 16 (1, 2, 4, 8 lanes on),
+// then the last of a row to the next one's, then lane 31 to the upper half.  (All
+// lanes active.  By shuffles each step is a trip through LDS.)
+__device__ __forceinline__ int lane_sum(int x) {
+  x = step_sum<0x111, 0xf>(x);
+  x = step_sum<0x112, 0xf>(x);
+  x = step_sum<0x114, 0xf>(x);
+  x = step_sum<0x118, 0xf>(x);
+  x = step_sum<0x142, 0xa>(x);
+  return step_sum<0x143, 0xc>(x);
+}
+__device__ __forceinline__ int2 lane_sums(int2 x) { return make_int2(lane_sum(x.x), lane_sum(x.y)); }
 
 // The sums of the threads' x in front of this one, and of all (in `all`); for
 // the whole workgroup, of whole waves.
@@ -190,13 +196,8 @@ __global__ void __launch_bounds__(PL_THREADS) plan_update_kernel(PlanArgs a, int
         if (lane == 0) counts[u * waves + wave] = (int)__popcll(held);
       }
       __syncthreads();
-      int sum = lane < PL_EACH * waves ? counts[lane] : 0;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(sum, d);
-        sum += lane >= d ? y : 0;
-      }
-      const int before = sum - (lane < PL_EACH * waves ? counts[lane] : 0);
+      const int held = lane < PL_EACH * waves ? counts[lane] : 0;
+      const int sum = lane_sum(held), before = sum - held;
 #pragma unroll
       for (int u = 0; u < PL_EACH; ++u) {
         const int64_t at = (int64_t)count + __shfl(before, u * waves + wave) + rank[u];
@@ -386,10 +387,20 @@ template <typename T> struct Weights {
   }
 };
 
-template <typename F> __device__ __forceinline__ double wave_sum(F x) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
-  return x;
+// The sum up to and with this lane's, in a wave (steps as lane_sum's).
+template <int CTRL, int ROWS> __device__ __forceinline__ double step_sum(double x) {
+  const uint64_t u = (uint64_t)__double_as_longlong(x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)u, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, ROWS, 0xf, false);
+  return x + __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+__device__ __forceinline__ double sum_up_to(double x) {
+  x = step_sum<0x111, 0xf>(x);
+  x = step_sum<0x112, 0xf>(x);
+  x = step_sum<0x114, 0xf>(x);
+  x = step_sum<0x118, 0xf>(x);
+  x = step_sum<0x142, 0xa>(x);
+  return step_sum<0x143, 0xc>(x);
 }
 
 template <typename T>
@@ -412,9 +423,9 @@ __global__ void __launch_bounds__(VD_THREADS) verify_sums_kernel(VerifyArgs a) {
       rest += x;
       all += y;
     });
-  rest = wave_sum(rest);
-  all = wave_sum(all);
-  if ((tid & 63) == 0) {
+  rest = sum_up_to(rest);
+  all = sum_up_to(all);
+  if ((tid & 63) == 63) {
     part[0][tid >> 6] = rest;
     part[1][tid >> 6] = all;
   }
@@ -433,17 +444,6 @@ __global__ void __launch_bounds__(VD_THREADS) verify_sums_kernel(VerifyArgs a) {
 // threads: 24 us for 64 sequences.)
 constexpr int VD_EACH = 16;
 constexpr int VD_SPAN = VD_THREADS * VD_EACH;
-
-// The sum up to and with this lane's, in a wave.
-__device__ __forceinline__ double sum_up_to(double x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const double y = __shfl_up(x, d);
-    x += lane >= d ? y : 0.0;
-  }
-  return x;
-}
 
 template <typename T>
 __global__ void __launch_bounds__(VD_THREADS) verify_finalize_kernel(VerifyArgs a) {
