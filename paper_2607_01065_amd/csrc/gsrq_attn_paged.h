@@ -717,7 +717,9 @@ inline gsrq_status pt_plan(const gsrq_paged_attn* s, const gsrq_pages* pages, bo
   if (s->T > INT32_MAX / 2 || s->T * GQ > INT32_MAX / 2 || pages->B > (1 << 20))
     return GSRQ_E_UNSUPPORTED;
   const int64_t Hkv = pages->Hkv, B = pages->B, held = (int64_t)pages->per * pages->page_size;
-  // (8-bit pages: a sequence's few rows see no more than the window and themselves)
+  // (8-bit pages: a sequence's few rows see no more than the window and themselves;
+  // pieces by the table's length took 33 us for 16 x 5 drafts in a window of 4096,
+  // by the window 26)
   const int64_t cap = eight && s->window ? std::min<int64_t>(held, (int64_t)s->window + PT_FEW) : held;
   // `few`: pieces that give every CU two workgroups, and where they stay longer
   // than 512 keys twice as many (lengths differ); of one round of the four waves
