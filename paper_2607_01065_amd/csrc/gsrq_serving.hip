@@ -551,7 +551,7 @@ __global__ void __launch_bounds__(VD_MOST) verify_row_kernel(VerifyArgs a) {
   const int row = stop_of<T>(a, b, first, rejected);
   if (tid == 0) {
     a.accepted[b] = row < 0 ? 0 : row - first;
-    a.next[b] = -1;
+    if (row < 0) a.next[b] = -1;
     hit = INT32_MAX;
     last = -1;
   }
@@ -582,7 +582,9 @@ __global__ void __launch_bounds__(VD_MOST) verify_row_kernel(VerifyArgs a) {
     if (from + up > point) atomicMin(&hit, tid);
   }
   __syncthreads();
-  if (tid != (hit < INT32_MAX ? hit : last)) return;
+  const int who = hit < INT32_MAX ? hit : last;
+  if (who < 0 && tid == 0) a.next[b] = -1;
+  if (tid != who) return;
   // the token that passes the point, or the last of any weight
   double at = from + (lane ? in : 0.0);
   int here = -1, heavy = 0;
