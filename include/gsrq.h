@@ -692,6 +692,8 @@ gsrq_status gsrq_verify_drafts_workspace_bytes(int64_t T, int64_t V, int32_t B, 
  *  uniform, draw     [T], [B] float32 numbers of [0, 1).
  *  q_start           [B + 1] int32, ascending, inside [0, T].
  *  accepted          [B] int32: drafts accepted (0 for a sequence without rows).
+ *                    Of n > 0 rows, n - 1 - accepted go back (gsrq_paged_plan);
+ *                    of a sequence that was not served, nothing does.
  *  next              [B] int32: the token after them; -1 for a sequence without
  *                    rows and where no weight is above zero.
  *  workspace         >= gsrq_verify_drafts_workspace_bytes(T, V, B), 256-byte

@@ -972,7 +972,8 @@ def verify_drafts(tokens, target, draft, uniform, draw, q_start, *, accepted=Non
     row, float32, float16 or bfloat16, rows at any stride; uniform [T] and
     draw [B] float32 numbers of [0, 1); q_start [B + 1] int32.  Returns
     (accepted [B], next token [B]) int32, new tensors or those given.  With n
-    rows of a sequence, paged_plan takes its n - 1 - accepted other drafts back."""
+    rows of a sequence (as q_start has them, not as it asked for), paged_plan
+    takes its n - 1 - accepted other drafts back; none where n is 0."""
     torch = _torch()
     lib = _lib or load_library()
     if target.dim() != 2:

@@ -381,3 +381,82 @@ def test_readme_example_of_8_bit_pages():
     assert names["accepted"].tolist() == ref[0].tolist() and names["next_token"].tolist() == ref[1].tolist()
     assert names["seq_len"].tolist() == [1 + a for a in names["accepted"].tolist()]
     assert int(names["n_free"]) == 12 - sum(-(-(1 + a) // 16) for a in names["accepted"].tolist())
+
+
+def test_readme_step_leaves_sequences_that_were_not_served():
+    """The README's step once more, for a sequence that grows, one that asks for more pages than are free and one that brings
+    nothing: the lengths, pages and the list of those that got no rows stay as they are."""
+    import os
+    import re
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    block = next(b for b in re.findall(r"```python\n(.*?)```", text, re.S) if "verify_drafts" in b)
+    at = block.index("# `new` [n]")
+    n, Hkv, V = 3, 2, 300
+    g = torch.Generator(device="cuda").manual_seed(11)
+    names = dict(torch=torch, B=B, n=n, per=4, pages=5, Hkv=Hkv, theta=10000.0 ** (torch.arange(64, dtype=torch.float64, device="cuda") * (-2.0 / 128)))
+    exec(block[:at], names)
+
+    def step(new):
+        T = sum(new)
+        k, v, q = (torch.randn((T, h, 128), generator=g, device="cuda").half() for h in (Hkv, Hkv, 4))
+        target, draft = (torch.rand((T, V), generator=g, device="cuda") for _ in range(2))
+        names.update(T=T, new=_i32(new), k=k, v=v, q=q, target=target, draft=draft, tokens=torch.randint(0, V, (T,), generator=g, device="cuda").int(),
+                     uniform=torch.zeros(T, device="cuda"), draw=torch.rand(n, generator=g, device="cuda"))
+        exec(block[at:], names)
+        return names["accepted"].tolist()
+
+    assert step([4, 18, 9]) == [3, 17, 8]                      # (every draft stands)
+    state = [names[x] for x in ("table", "free", "n_free", "seq_len")]
+    assert state[3].tolist() == [4, 18, 9] and int(state[2]) == 1
+    table = state[0].tolist()
+    assert step([3, 40, 0]) == [2, 0, 0]
+    assert names["q_start"].tolist() == [0, 3, 3, 3] and names["next_token"].tolist()[1:] == [-1, -1]
+    assert state[3].tolist() == [7, 18, 9] and state[0].tolist() == table and int(state[2]) == 1
+    assert step([1, 14, 0])[1] == 13 and state[3].tolist() == [8, 32, 9]    # (and it goes on from there)
+
+
+def test_captured_step_whose_pages_run_short():
+    """A step in a graph, replayed until the list is empty, against eager calls on a copy of the state and lists on the host:
+    a sequence that was not served keeps its length and pages."""
+    n, drafts, V, page, F, per = 4, 3, 500, 8, 14, 12
+    rows = n * (1 + drafts)
+    g = torch.Generator().manual_seed(2)
+    lens = [8, 15, 1, 16]                                  # (6 of 14 pages)
+    host, eager = (Batch(n, per, page, F, lens, seed=5) for _ in range(2))
+    held = [x.clone() for x in eager.dev]
+    p, q = (torch.rand((rows, V), generator=g).cuda() for _ in range(2))
+    u, d, grow = torch.zeros(rows, device="cuda"), torch.zeros(n, device="cuda"), _i32([1 + drafts] * n)
+    tokens = torch.randint(0, V, (rows,), generator=g).int().cuda()
+
+    def step(s):
+        start, slots, positions = B.paged_plan(*s, grow, page_size=page, rows=rows)
+        accepted, token = B.verify_drafts(tokens, p, q, u, d, start)
+        got = start[1:] - start[:-1]
+        B.paged_plan(*s, torch.where(got > 0, accepted - (got - 1), 0), page_size=page, rows=0)
+        return [start, slots, positions, accepted, token]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step([x.clone() for x in held])
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step(held)
+    short = 0
+    for _ in range(12):
+        u.copy_(torch.rand(rows, generator=g))
+        d.copy_(torch.rand(n, generator=g))
+        before = list(host.lens)
+        want = step(eager.dev)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(captured + held, want + eager.dev))
+        host.step([1 + drafts] * n, rows)
+        new = [x - y for x, y in zip(host.lens, before)]
+        ref = C.verify(tokens.cpu(), p.cpu(), q.cpu(), u.cpu(), d.cpu(), want[0].cpu())
+        assert want[3].tolist() == ref[0].tolist() and want[4].tolist() == ref[1].tolist()
+        host.step([a - (m - 1) if m else 0 for a, m in zip(ref[0].tolist(), new)], 0)
+        assert held[3].tolist() == host.lens and held[0].tolist() == host.table
+        short += new.count(0)
+    assert short                                           # (the list did run short)
