@@ -102,17 +102,6 @@ template <typename TI> struct Raw {
   }
 };
 
-// 1 / sqrt(mean square + eps) of a head, in F; its L lanes all active.
-template <typename F, int HD>
-__device__ __forceinline__ F norm_factor(const float (&lo)[8], const float (&hi)[8], float eps) {
-  F ss = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) ss = fma((F)lo[j], (F)lo[j], fma((F)hi[j], (F)hi[j], ss));
-#pragma unroll
-  for (int m = 1; m < HD / 16; m <<= 1) ss += __shfl_xor(ss, m);
-  return (F)1 / sqrt(ss * ((F)1 / HD) + (F)eps);
-}
-
 template <typename F> __device__ __forceinline__ void turned(F& lo, F& hi, F c, F s) {
   const F x = lo, y = hi;
   lo = x * c - y * s;
@@ -173,7 +162,7 @@ __device__ __forceinline__ void exact_sizes(const PageRows<TI>& w, unsigned long
       float lo[8], hi[8];
       x.load(src + 8 * l, HD / 2);
       x.get(lo, hi);
-      r = norm_factor<double, HD>(lo, hi, w.eps);
+      r = 1.0 / sqrt(sum_of_squares<double, HD>(lo, hi) * (1.0 / HD) + (double)w.eps);
     }
 #pragma unroll 1
     for (int j = 8 * l; j < 8 * l + 8; ++j) {
@@ -258,20 +247,22 @@ __device__ __forceinline__ void append_page(const Append8Args& a, int64_t wg) {
     h = wide ? head0 + i * beside : i % w.heads;
     return i < items && t < w.tokens && h < w.heads && (!wide || head0 < beside);
   };
-  // `factor`: of the norm, taken where it is `unknown`
+  // `factor`: of the norm, taken where it is `unknown` (or below zero)
   auto numbers_of = [&](const Raw<TI>& x, int t, int& turned_to, Turns& turns, bool kept,
                         bool unknown, float& factor, float (&lo)[8], float (&hi)[8])
                         __attribute__((always_inline)) {
     asm volatile("" : : : "memory");                   // (weights are read anew, not kept in registers)
     x.get(lo, hi);
     if (w.norm) {
-      if (unknown) factor = norm_factor<float, HD>(lo, hi, w.eps);
+      bool scaled = false;
+      if (unknown || factor < 0.f) factor = norm_factor<HD>(lo, hi, w.eps, scaled);
       const float r = factor;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         lo[j] *= r * weight[8 * l + j];
         hi[j] *= r * weight[HALF + 8 * l + j];
       }
+      if (scaled) factor = -1.f;                       // (taken anew, with the elements' scaling)
     }
     if (w.theta) {
       if (t != turned_to) {
@@ -458,7 +449,8 @@ __device__ __forceinline__ void append_queries(const Append8Args& a, int64_t wg)
     float lo[8], hi[8];
     x[i].get(lo, hi);
     if (a.q_norm) {
-      const float r = norm_factor<float, HD>(lo, hi, a.eps);
+      bool scaled;
+      const float r = norm_factor<HD>(lo, hi, a.eps, scaled);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         lo[j] *= r * a.q_norm[8 * l + j];

@@ -142,6 +142,36 @@ __device__ __forceinline__ void store8(__bf16* p, const float (&x)[8]) {
   *(b8*)p = v;
 }
 
+// The sum of a head's squares, in F; its HD / 16 lanes (16 elements each) all active.
+template <typename F, int HD>
+__device__ __forceinline__ F sum_of_squares(const float (&lo)[8], const float (&hi)[8]) {
+  F ss = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) ss = fma((F)lo[j], (F)lo[j], fma((F)hi[j], (F)hi[j], ss));
+#pragma unroll
+  for (int m = 1; m < HD / 16; m <<= 1) ss += __shfl_xor(ss, m);
+  return ss;
+}
+
+// 1 / sqrt(mean square + eps) of a head.  Where float32 does not hold the squares (elements from
+// 2^60 on, or a mean and eps below 2^-100 together), the elements are scaled, by a power of two,
+// and the factor is that of the scaled ones: their product is the same.
+template <int HD>
+__device__ __forceinline__ float norm_factor(float (&lo)[8], float (&hi)[8], float eps, bool& scaled) {
+  float t = sum_of_squares<float, HD>(lo, hi) * (1.f / HD) + eps;
+  scaled = !(t >= 0x1p-100f && t < INFINITY);
+  if (__builtin_expect(scaled, 0)) {
+    const float s = t < 1.f ? 0x1p100f : 0x1p-72f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      lo[j] *= s;
+      hi[j] *= s;
+    }
+    t = sum_of_squares<float, HD>(lo, hi) * (1.f / HD) + eps * s * s;
+  }
+  return 1.f / sqrtf(t);
+}
+
 // Cosine and sine of pos * theta.  In 64 bits up to the whole turns: at
 // position 2^20 a float32 product would be off by 0.06 radians.
 __device__ __forceinline__ void turn_of(int64_t pos, double theta, float& c, float& s) {

@@ -192,6 +192,22 @@ def test_exponents_at_their_borders():
         _check_append(k, k, None, *_pools(per, 8, 1, hd, "token"), R.table(1, per, per), one, torch.tensor([pos + 1], dtype=torch.int32), theta)
 
 
+SIZES = (1.0, 2.0 ** 62, 2.0 ** 64, 2.0 ** 100, 2.0 ** 124, 2.0 ** -48, 2.0 ** -52, 2.0 ** -64, 2.0 ** -80, 2.0 ** -110, 2.0 ** -130)
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-6, 2.0 ** -104, 2.0 ** 110])
+@pytest.mark.parametrize("src,tokens,Hkv,hd,page,rope", [("f32", 33, 3, 64, 64, True), ("bf16", 33, 2, 128, 16, True), ("bf16", 11, 1, 256, 8, False),
+                                                         ("f32", 77, 1, 256, 128, True)])
+def test_norms_of_rows_whose_squares_leave_float32(src, tokens, Hkv, hd, page, rope, eps):
+    """Rows of 2^-130 to 2^124 next to each other, whose sums of squares float32 does not hold: normed like any others."""
+    start, k, v, q, w = _rows([tokens], 2 * Hkv, Hkv, hd, torch.float32, spread=1.0)
+    size = torch.tensor(SIZES)[torch.arange(tokens) % len(SIZES)][:, None, None]
+    k, q = (torch.randn(x.shape, generator=torch.Generator().manual_seed(i)) * size for i, x in enumerate((k, q)))
+    per = -(-(tokens + 5) // page)
+    _check_append(k.to(R.TYPES[src]), v.to(R.TYPES[src]), q.to(R.TYPES[src]), *_pools(per + 1, page, Hkv, hd, "token"), R.table(1, per, per + 1), start,
+                  torch.tensor([tokens + 5], dtype=torch.int32), _theta(hd) if rope else None, *w, eps=eps)
+
+
 def test_far_positions_strided_rows_and_strided_exponents():
     """Positions near 2^30, k, v, q as slices of one projection's rows, exponents of keys and values side by side."""
     hd, page, Hkv = 64, 1 << 14, 2
