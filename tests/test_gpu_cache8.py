@@ -208,6 +208,54 @@ def test_norms_of_rows_whose_squares_leave_float32(src, tokens, Hkv, hd, page, r
                   torch.tensor([tokens + 5], dtype=torch.int32), _theta(hd) if rope else None, *w, eps=eps)
 
 
+@pytest.mark.parametrize("src,out,counts,lens,Hq,Hkv,hd,page,order", [
+    ("bf16", "bf16", [100, 130], [100, 200], 4, 2, 256, 128, "token"),
+    ("f16", "f16", [200], [237], 2, 1, 128, 256, "head"),
+    ("f32", "f16", [300], [300], 3, 3, 64, 512, "token"),
+])
+def test_norms_and_turns_in_pages_longer_than_what_is_kept(src, out, counts, lens, Hq, Hkv, hd, page, order):
+    """More new tokens in a page than stay in registers, normed and turned; from the page's first token on and from inside it."""
+    per = -(-max(lens) // page)
+    pages = len(counts) * per + 1
+    start, k, v, q, w = _rows(counts, Hq, Hkv, hd, R.TYPES[src])
+    q_out = torch.empty(q.shape, dtype=R.TYPES[out], device="cuda")
+    _check_append(k, v, q, *_pools(pages, page, Hkv, hd, order), R.table(len(counts), per, pages), start,
+                  torch.tensor(lens, dtype=torch.int32), _theta(hd), *w, out=q_out)
+
+
+def test_exponents_at_their_borders_after_norm_and_turn():
+    """Pairs in directions that the turn takes onto an axis: normed
+    and turned, the largest is 448 to within float32, or a little to either side."""
+    hd = 64
+    theta, one = _theta(hd), torch.tensor([0, 1], dtype=torch.int32)
+    for pos in (0, 8, 80, 4000):                               # (pages that start anew)
+        a = pos * theta
+        k = torch.cat([torch.cos(a), -torch.sin(a)]).float().view(1, 1, hd)
+        per = pos // 8 + 1
+        for step in (0.0, 2.0 ** -23, -(2.0 ** -22), 2.0 ** -18):
+            w = torch.full((hd,), 448.0 / math.sqrt(2) * (1 + step))
+            got = _check_append(k * 3, k, None, *_pools(per, 8, 1, hd, "token"), R.table(1, per, per), one, torch.tensor([pos + 1], dtype=torch.int32),
+                                theta, w, eps=0.0)[2]
+            assert int(got[int(R.table(1, per, per)[0, pos // 8]), 0]) in (0, 1)
+
+
+def test_a_coded_session_into_8_bit_pages():
+    """decode() and paged_append(): what a 1-bit cache holds, turned and in 8-bit pages."""
+    T, Hkv, hd, page = 300, 2, 128, 16
+    g = torch.Generator().manual_seed(3)
+    rows = []
+    for i in range(2):
+        x = torch.randn((T, Hkv * hd), generator=g).half().cuda()
+        seeds = torch.stack([torch.randperm(T, generator=g)[:256] for _ in range(Hkv * hd // 8)]).int().numpy()
+        r = B.train_stage(x, d=8, K=256, T=3, seed_rows=seeds)
+        codes, _ = B.encode(x, r.gain[None], r.shape[None])
+        rows.append(B.decode(codes, r.gain[None], r.shape[None], Hkv * hd).view(T, Hkv, hd).cpu())
+    assert float(rows[0].abs().max()) > 0
+    per = -(-T // page)
+    _check_append(*rows, None, *_pools(per + 1, page, Hkv, hd, "token"), R.table(1, per, per + 1), torch.tensor([0, T], dtype=torch.int32),
+                  torch.tensor([T], dtype=torch.int32), _theta(hd))
+
+
 def test_far_positions_strided_rows_and_strided_exponents():
     """Positions near 2^30, k, v, q as slices of one projection's rows, exponents of keys and values side by side."""
     hd, page, Hkv = 64, 1 << 14, 2
