@@ -77,12 +77,8 @@ __global__ void __launch_bounds__(PA_THREADS) paged_append_kernel(AppendArgs a) 
   load8(src + 8 * l, lo);
   load8(src + HD / 2 + 8 * l, hi);
   if (norm) {
-    float ss = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) ss = fmaf(lo[j], lo[j], fmaf(hi[j], hi[j], ss));
-#pragma unroll
-    for (int m = 1; m < L; m <<= 1) ss += __shfl_xor(ss, m);
-    const float r = 1.f / sqrtf(ss * (1.f / HD) + a.eps);
+    bool scaled;
+    const float r = norm_factor<HD>(lo, hi, a.eps, scaled);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       lo[j] *= r * norm[8 * l + j];

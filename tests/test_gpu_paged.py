@@ -86,6 +86,24 @@ def test_append(src, held, counts, lens, Hq, Hkv, hd, page, order, rope, norm, g
         _close(dev[3], vd, vm, "v"))
 
 
+@pytest.mark.parametrize("eps", [0.0, 1e-6, 2.0 ** -104, 2.0 ** 110])
+@pytest.mark.parametrize("src,held,hd,rope", [("f32", "bf16", 64, True), ("bf16", "bf16", 128, True), ("f32", "f16", 256, False)])
+def test_append_norms_of_rows_whose_squares_leave_float32(src, held, hd, rope, eps):
+    """Rows of 2^-130 to 2^124 next to each other, whose sums of squares float32 does not hold: normed like any others."""
+    sizes = torch.tensor((1.0, 2.0 ** 62, 2.0 ** 64, 2.0 ** 100, 2.0 ** 124, 2.0 ** -48, 2.0 ** -52, 2.0 ** -64, 2.0 ** -80, 2.0 ** -110, 2.0 ** -130))
+    T, Hkv, Hq, page = 33, 2, 3, 16
+    start, k, v, q, w = _inputs([T], Hq, Hkv, hd, torch.float32)
+    k, q = ((torch.randn(x.shape, generator=torch.Generator().manual_seed(i)) * sizes[torch.arange(T) % 11][:, None, None]).to(R.TYPES[src])
+            for i, x in enumerate((k, q)))
+    v = v.to(R.TYPES[src])
+    kp, vp = (R.pool(4, page, Hkv, hd, R.TYPES[held], "token", s) for s in (1, 2))
+    tab, lens, theta = R.table(1, 3, 4), torch.tensor([T + 5], dtype=torch.int32), _theta(hd) if rope else None
+    qd, kd, vd, qm, km, vm = R.append(k, v, kp, vp, tab, start, lens, q, theta, *w, eps=eps)
+    dev = [t.cuda() for t in (k, v, kp, vp, tab, start, lens)]
+    got = B.paged_append(*dev, q=q.cuda(), theta=None if theta is None else theta.cuda(), k_norm=w[0].cuda(), q_norm=w[1].cuda(), eps=eps)
+    say("worst share of the tolerance", _close(got, qd, qm, "q"), _close(dev[2], kd, km, "k"), _close(dev[3], vd, vm, "v"))
+
+
 def test_append_far_positions_and_strided_rows():
     """Positions near 2^30, and k, v, q as slices of one projection's rows."""
     Hq, Hkv, hd, page, per = 4, 2, 128, 1 << 14, 1 << 16
