@@ -622,7 +622,7 @@ typedef struct {
   int64_t T;          /* rows that slots and positions have room for          */
   int64_t ldt;        /* entries from row to row of the table (>= per)        */
   int32_t B;          /* sequences, at most 8192                              */
-  int32_t per;        /* table entries per sequence                           */
+  int32_t per;        /* table entries per sequence (B * per < 2^31 - 4096)    */
   int32_t page_size;  /* tokens per page (as gsrq_pages)                      */
   int32_t F;          /* entries of the free list: as many as the pool's pages */
 } gsrq_paged_batch;

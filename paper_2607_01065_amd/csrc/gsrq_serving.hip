@@ -646,7 +646,9 @@ gsrq_status gsrq_paged_plan(const gsrq_paged_batch* s, int32_t* table, int32_t* 
   if (s->T > 0 && (!slots || !positions)) return GSRQ_E_ARG;
   if ((int64_t)s->page_size * s->per > (1 << 30)) return GSRQ_E_ARG;
   if (!is_pow2(s->page_size) || s->page_size < 8) return GSRQ_E_UNSUPPORTED;
-  if (s->B > PL_MOST || s->T > INT32_MAX / 2 || (int64_t)s->B * s->per > INT32_MAX)
+  // (a round of moved entries behind the last is still counted in 32 bits)
+  if (s->B > PL_MOST || s->T > INT32_MAX / 2 ||
+      (int64_t)s->B * s->per > INT32_MAX - PL_THREADS * PL_EACH)
     return GSRQ_E_UNSUPPORTED;
   PlanArgs a;
   a.table = table;

@@ -197,3 +197,10 @@ def test_binding_verify_refuses():
                       (dict(accepted=torch.zeros(3, **i32)), ValueError), (dict(next_token=torch.zeros(2)), TypeError), (dict(), ValueError)):
         with pytest.raises(error):
             B.verify_drafts(**{**good, **kw})
+
+
+@pytest.mark.parametrize("Bn,per", [(8191, 262176), (1023, 2099202), (17, 126322567)])
+def test_plan_refuses_tables_whose_entries_cannot_be_counted_in_rounds(Bn, per):
+    """Just below 2^31 entries: the counter of a round of 4096 moves would wrap and never end."""
+    assert (1 << 31) - 4096 <= Bn * per < 1 << 31
+    assert _plan(Bn=Bn, per=per, ldt=per, page=8) == 2
