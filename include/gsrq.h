@@ -552,7 +552,7 @@ typedef struct {
  * where they have raised it.
  *
  * A page that a call writes from two rows of the table holds anything
- * afterwards.
+ * afterwards.  A page's keys take less than 2^35 - 2^12 bytes.
  *
  *  q_out, q_dtype    queries [T][Hq][head_dim], float16 or bfloat16; q_out may
  *                    be q itself where the types agree and q is dense.

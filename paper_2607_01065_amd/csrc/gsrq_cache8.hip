@@ -1233,6 +1233,9 @@ gsrq_status gsrq_paged_append8(const gsrq_pages* pages, const gsrq_page_exps* ex
   if (T > MAX_BLOCKS || a.pool.B > (1 << 20)) return GSRQ_E_UNSUPPORTED;
   if (2ll * a.pool.Hkv + (q ? Hq : 0) > 65535) return GSRQ_E_UNSUPPORTED;
   const int hd = pages->head_dim, rows = E8_THREADS * 16 / hd;
+  // (a page's codes are rounded again 16 bytes a thread, counted in 32 bits)
+  if ((int64_t)pages->page_size * (a.pool.Hkv * (hd / 16)) > INT32_MAX - E8_THREADS)
+    return GSRQ_E_UNSUPPORTED;
   // as many heads as E8_KEEP items a thread hold of a page's tokens; fewer where that
   // leaves less than 512 workgroups, but for sequences of one token each, whose
   // heads are few items (512 tokens: 11.9 us with all, 8.7 so; 32 sequences of one

@@ -204,3 +204,10 @@ def test_plan_refuses_tables_whose_entries_cannot_be_counted_in_rounds(Bn, per):
     """Just below 2^31 entries: the counter of a round of 4096 moves would wrap and never end."""
     assert (1 << 31) - 4096 <= Bn * per < 1 << 31
     assert _plan(Bn=Bn, per=per, ldt=per, page=8) == 2
+
+
+@pytest.mark.parametrize("kw", [dict(page_size=1 << 25), dict(page_size=1 << 24, head_dim=256), dict(page_size=1 << 26, head_dim=64),
+                                dict(page_size=1 << 30, Hkv=4, head_dim=64)])
+def test_append_refuses_pages_whose_codes_cannot_be_counted(kw):
+    """Pages of 2^31 pieces of 16 bytes and more: the counter of the codes that are rounded again would wrap."""
+    assert _append(_p(per=1, ldt=1, pages=1, **kw)) == 2
