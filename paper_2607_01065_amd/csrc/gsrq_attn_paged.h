@@ -17,6 +17,7 @@ constexpr int PT_FEW = 32;                 // queries per key head of the `few` 
 constexpr int PT_FEW_UNIT = 32 * PT_WAVES; // keys of one round of its four waves
 constexpr float PT_HEADROOM = 8.f;         // log2 by which a tile may exceed the maximum in use
 constexpr float PT_SHIFT = 6.f;            // log2 of the largest weight at a fresh maximum
+static_assert(PT_HEADROOM + PT_SHIFT < 16.f, "weights are float16 numbers");
 
 typedef __attribute__((address_space(3))) char lds_char;
 typedef _Float16 h4 __attribute__((ext_vector_type(4)));

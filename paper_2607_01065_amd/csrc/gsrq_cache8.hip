@@ -14,11 +14,12 @@
 // products, pieces joined by a second launch); with the scales out of the
 // products: for the codes c of keys and d of values, and their exponents,
 //   s_j = (scale 2^ek) q . c_j,   o = sum_j w_j d_j / sum_j w_j 2^-ev,
-//   w_j = 2^(s_j log2(e) + ev - m),   m = the running maximum of s_j log2(e) + ev.
+//   w_j = 2^(s_j log2(e) + ev - m + 6),   m = a running maximum of s_j log2(e) + ev.
 // One subtraction and one factor per page and tile take the place of a product
-// per element, w_j is at most 1 whatever the scales, and the float16 rounding of
-// w_j is relative to the largest product of weight and scale.  Codes are exact
-// in float16 and bfloat16.
+// per element.  m is raised only by a tile that exceeds it by 2^8, so w_j is at
+// most 2^14 whatever the scales (float16 ends at 65504), and its float16 rounding is
+// relative to the largest product of weight and scale.  Codes are exact in
+// float16 and bfloat16.
 #include "gsrq_attn_paged.h"
 
 namespace {
@@ -739,8 +740,11 @@ template <int ROWS> __device__ __forceinline__ uint64_t gone_rows(uint32_t group
 }
 
 // As load_to_lds(), from an address of the lane's own, and past the caches: keys and
-// values of few rows are read once (8 sequences of <= 32768 tokens: 94 us a call,
-// 104 with cached loads; 16 of 60000 5.5 TB/s and 5.1).
+// values of few rows are read once (8 sequences of <= 32768 tokens, 32 / 8 heads of
+// 128: 92 us a call, 102 with cached loads; of 256: 167 and 182).  Not so with heads of
+// 64, whose row is half a cache line and the other half another workgroup's: there
+// cached loads are the faster (54 us, 61 so).  Sixteen sequences that share the pages
+// of 16000 tokens: the same with heads of 128 (67 us and 67) and of 64 (55 and 55).
 __device__ __forceinline__ void load_lane_to_lds(const char* at, uint32_t to) {
   asm volatile(
       "s_mov_b32 m0, %1\n\t"
@@ -1145,7 +1149,8 @@ __device__ __forceinline__ void few8(const Pt8Args& a8, char* lds, int block) {
 }
 
 // (Two workgroups a CU also for heads of 64: in the registers of three, chunks
-// spill; 1024 tokens over 30000 took 291 us against 228.)
+// spill; 1024 tokens over 30000 took 540 us against 437 with 32 / 8 heads, 289 against
+// 228 with 16 / 16.)
 template <typename T, int HD>
 __global__ void __launch_bounds__(PT_THREADS, HD == 256 ? 1 : 2) cache8_attn_kernel(Pt8Args a) {
   __shared__ __align__(16) char lds[Pt8Cfg<HD>::LDS];
@@ -1238,8 +1243,10 @@ gsrq_status gsrq_paged_append8(const gsrq_pages* pages, const gsrq_page_exps* ex
     return GSRQ_E_UNSUPPORTED;
   // as many heads as E8_KEEP items a thread hold of a page's tokens; fewer where that
   // leaves less than 512 workgroups, but for sequences of one token each, whose
-  // heads are few items (512 tokens: 11.9 us with all, 8.7 so; 32 sequences of one
-  // token 6.5 and 7.8)
+  // heads are few items (8 heads of 128, kernel times: 512 tokens of one sequence 9.8 us
+  // with all, 7.7 so; 32 sequences of one token 5.6 and 7.0).  Sequences of a few drafts
+  // are few items too, and lose by it: 32 of 5 tokens take 9.0 us, with all heads 6.4;
+  // 128 of 5 11.3 and 8.4.
   const int tokens = (int)std::min<int64_t>(pages->page_size, T);
   const int most = tokens <= rows ? E8_KEEP * (rows / tokens) : E8_KEEP / ((tokens + rows - 1) / rows);
   const int64_t touched = (T >> a.pool.shift) + a.pool.B;

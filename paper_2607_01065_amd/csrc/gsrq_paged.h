@@ -155,7 +155,9 @@ __device__ __forceinline__ F sum_of_squares(const float (&lo)[8], const float (&
 
 // 1 / sqrt(mean square + eps) of a head.  Where float32 does not hold the squares (elements from
 // 2^60 on, or a mean and eps below 2^-100 together), the elements are scaled, by a power of two,
-// and the factor is that of the scaled ones: their product is the same.
+// and the factor is that of the scaled ones: their product is the same.  (The
+// comparison costs appending to 8-bit pages 1%: 20000 rows of 32 / 8 heads of 128 take
+// 101.3 us, 100.3 without; to 16-bit pages nothing, 94.)
 template <int HD>
 __device__ __forceinline__ float norm_factor(float (&lo)[8], float (&hi)[8], float eps, bool& scaled) {
   float t = sum_of_squares<float, HD>(lo, hi) * (1.f / HD) + eps;

@@ -4,8 +4,10 @@
 // Planning.  Sequence b of L tokens changes by c tokens, L' = max(L + c, 0), and
 // needs ceil(L' / P) pages.  Pages given back go on the free list, those needed
 // come from it; who gets which is an exclusive sum over the batch.  The whole
-// batch is one workgroup's (a few reads and sums per sequence: the time is that of
-// a launch), the rows' slots a second launch's.
+// batch is one workgroup's: a few reads and sums per sequence (32 sequences of one
+// token: 3 us), and rounds of reads and stores per page that moves (8600 pages: 12 us
+// taking them, 16 giving them back).  Up to 2048 rows it writes their slots too; those
+// of more rows are a second launch's.
 //
 // Verification.  Row r of the target's probabilities p and the draft's q decides
 // about draft t: accepted iff u q(t) < p(t).  The first rejected row's token is
